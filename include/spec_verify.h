@@ -58,6 +58,12 @@ extern "C" {
 #define SPEC_FLAG_FREE_OVERFLOW 16 /* free list capacity exceeded in spec_kv_commit */
 #define SPEC_FLAG_NO_SEED 32      /* temperature > 0 but seeds == NULL */
 #define SPEC_FLAG_BAD_TREE 64     /* parent[] of a request is not a tree in topological order */
+#define SPEC_FLAG_NO_PAGES 128    /* spec_kv_reserve: the free list is too short for a request */
+#define SPEC_FLAG_BAD_KV 256      /* spec_kv_quantize: an infinity or a NaN in the rows (stored as 0) */
+
+/* element type of a cache that holds 8 bits per element */
+#define SPEC_KV_E4M3 0            /* OCP e4m3: 4 exponent bits, 3 fraction bits, largest value 448, no infinities */
+#define SPEC_KV_INT8 1            /* signed byte */
 
 /* Text of the calling thread's last error ("" if none). host. */
 const char* spec_last_error_string(void);
@@ -472,6 +478,96 @@ int spec_kv_commit_tree(void* k_cache, void* v_cache, int32_t* page_table, int m
                         const int32_t* path, int gamma_max,
                         int32_t* free_list, int32_t free_capacity, int32_t* free_count,
                         int B, int Hkv, int D, int page_size, int32_t* status_flags, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * spec_kv_reserve — pages and slots for the rows of the next pass (the other
+ * half of Commit's page accounting: the candidates' K/V enter the cache before
+ * they are verified, Appendix "Target side"; prompts likewise).
+ *   Request i gets pages for positions c_i .. c_i + n_i - 1 (lengths as above;
+ *   n_i = 0 asks for nothing): its unmapped (negative) entries of page_table
+ *   below ceil((c_i + n_i) / P) are filled from the END of free_list, whose last
+ *   entries keep their order: requests ascending, logical pages ascending.
+ *   (spec_kv_commit / spec_kv_truncate append in that order, so that a call
+ *   whose rows are all taken back leaves the free list as it was.)  Entries that
+ *   are mapped already are kept, so a repeated call takes nothing.  Requests are
+ *   served in order as far as the free list goes; one that cannot be served
+ *   whole, and those behind it that need a page, take none and raise
+ *   SPEC_FLAG_NO_PAGES.
+ *   slot_map[r], for row r = qo_indptr[i] + j: page * P + offset of position
+ *   c_i + j; -1 for the rows of requests that were not served and for rows of
+ *   no request (r >= qo_indptr[B]).
+ *   A request whose lengths do not fit (c_i < 0, n_i < 0, rows outside [0, M),
+ *   more than max_pages_per_seq pages) raises SPEC_FLAG_BAD_LENGTH; one with a
+ *   hole in its mapped pages, with committed tokens but no page for the last of
+ *   them, or with a mapped id >= num_pages raises SPEC_FLAG_BAD_PAGE: both are
+ *   not served.  A free-list entry outside [0, num_pages) is taken but not
+ *   entered (its rows get -1) and raises SPEC_FLAG_BAD_PAGE.
+ *   page_table [B, max_pages_per_seq] in/out; free_list [free_capacity] in;
+ *   free_count [1] in/out; slot_map [M] out, int32.  num_pages * page_size must
+ *   be below 2^31 (SPEC_ESHAPE).  workspace: spec_kv_reserve_workspace_bytes(B).
+ * ------------------------------------------------------------------------- */
+size_t spec_kv_reserve_workspace_bytes(int B);
+
+int spec_kv_reserve(int32_t* page_table, int max_pages_per_seq, int num_pages,
+                    const int32_t* seq_lens, const int32_t* qo_indptr,
+                    const int32_t* free_list, int32_t free_capacity, int32_t* free_count, int32_t* slot_map,
+                    int B, int M, int page_size, int32_t* status_flags,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache in 8 bits.  k_cache, v_cache [num_pages, Hkv, page_size, D] of
+ * kv_type elements (16-byte aligned), k_scale, v_scale [num_pages, Hkv] fp32: an element b of page p and kv
+ * head h stands for b * scale[p][h].  Page accounting (spec_kv_reserve,
+ * spec_kv_commit, spec_kv_truncate) is the same for both kinds of cache.  Built
+ * for D = 128, page_size = 16 (SPEC_ESHAPE otherwise).
+ *
+ * spec_kv_quantize — writes rows into the cache.  k, v: row r, kv head h, element d
+ *   at r * row_stride + h * D + d, bf16 (16-byte aligned, row_stride a multiple of
+ *   8 and >= Hkv * D: slices of a projection's output need no copy).  Row r goes to
+ *   slot slot_map[r] = page * page_size + offset; -1: it is not stored; any other
+ *   value outside the cache: not stored, SPEC_FLAG_BAD_PAGE.
+ *   Consecutive rows in consecutive slots of one page are a run.  Per run and kv
+ *   head, with o = the offset of its first slot:
+ *     old = scale of the page if o > 0 (the page holds tokens) and that is positive
+ *           and finite, else 0
+ *     new = max(old, the smallest power of two 2^e, e >= -126, with
+ *           max|x| <= 448 * 2^e (int8: 127 * 2^e)); 0 for rows that are all zero
+ *   Elements are x / new rounded to nearest even (0 for new = 0); where new > old the
+ *   o tokens before the run are rounded again (element * (old / new) in fp32); the
+ *   slots behind the run are left as they were.  So a page begins anew with its slot
+ *   0, and rows that verification rejected are overwritten by the next ones, but what
+ *   they did to the scale of a page that still holds tokens stays.
+ *   Infinities and NaN are stored as 0, do not count for the scale, and raise
+ *   SPEC_FLAG_BAD_KV.  A page that occurs in more than one run of a call, and
+ *   slots that occur twice, end with unspecified contents (nothing else is touched).
+ *
+ * spec_kv_dequantize — reads rows back: row r of k, v (bf16, laid out and strided as
+ *   above) = element * scale in fp32, rounded to bf16 once (exact for the scales
+ *   that spec_kv_quantize sets).  Rows with slot_map[r] = -1 are left as they were;
+ *   other slots outside the cache likewise, SPEC_FLAG_BAD_PAGE.
+ * M * Hkv must be below 2^27 (SPEC_ESHAPE).  Both are asynchronous on the stream and allocate nothing.
+ * ------------------------------------------------------------------------- */
+int spec_kv_quantize(const void* k, const void* v, int64_t row_stride, const int32_t* slot_map,
+                     void* k_cache, void* v_cache, float* k_scale, float* v_scale, int num_pages,
+                     int M, int Hkv, int D, int page_size, int kv_type, int32_t* status_flags, void* stream);
+
+int spec_kv_dequantize(const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale, int num_pages,
+                       const int32_t* slot_map, void* k, void* v, int64_t row_stride,
+                       int M, int Hkv, int D, int page_size, int kv_type, int32_t* status_flags, void* stream);
+
+/* spec_verify_attn_quantized — spec_verify_attn over a cache in 8 bits: the same operation (K_t and V_t are the values
+ * that the elements stand for; scales: any finite values >= 0), arguments, limits, flags and errors.  Products in bf16 (every element is
+ * a bf16 value), scales, scores, sums and accumulation in fp32; the probabilities, times V's scale, are rounded to bf16.
+ * Chains only: candidate trees need the bf16 cache.  At the positions that a request sees no element may be NaN (spec_kv_quantize
+ * writes none); the slots behind them, and unmapped pages' scales, may hold anything. */
+size_t spec_verify_attn_quantized_workspace_bytes(int B, int M, int Hq, int Hkv, int D, int max_kv_len, int max_q_len);
+
+int spec_verify_attn_quantized(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
+                               const int32_t* page_table, int max_pages_per_seq, int num_pages,
+                               const int32_t* seq_lens, const int32_t* qo_indptr, void* out, float* lse,
+                               int B, int M, int Hq, int Hkv, int D, int page_size, int kv_type,
+                               int max_kv_len, int max_q_len, float scale, int32_t* status_flags,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Measurement probes (not part of the verification path; no passage of the paper defines them).  They give the

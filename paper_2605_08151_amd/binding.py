@@ -35,10 +35,12 @@ EXPORTS = (
     "spec_lm_head_packed_stats_blocks", "spec_lm_head_packed_stats",
     "spec_probe_read", "spec_probe_read_pages", "spec_probe_mfma", "spec_accept_static",
     "spec_lm_head_packed_summary_blocks", "spec_lm_head_packed_summary", "spec_accept_summary",
+    "spec_kv_reserve_workspace_bytes", "spec_kv_reserve", "spec_kv_quantize", "spec_kv_dequantize",
+    "spec_verify_attn_quantized_workspace_bytes", "spec_verify_attn_quantized",
 )
 
 FLAG_BAD_PAGE, FLAG_BAD_LENGTH, FLAG_BAD_LOGITS, FLAG_BAD_TOKEN, FLAG_FREE_OVERFLOW, FLAG_NO_SEED = 1, 2, 4, 8, 16, 32
-FLAG_BAD_TREE = 64
+FLAG_BAD_TREE, FLAG_NO_PAGES, FLAG_BAD_KV = 64, 128, 256
 
 
 class SpecError(RuntimeError):
@@ -51,7 +53,7 @@ def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python -c 'import __graft_entry__ as g; g.build()'`")
     lib = ctypes.CDLL(LIB_PATH)
-    vp, i32, f32, u32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint32, ctypes.c_size_t
+    vp, i32, i64, f32, u32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_uint32, ctypes.c_size_t
     lib.spec_last_error_string.restype = ctypes.c_char_p
     lib.spec_last_error_string.argtypes = []
     lib.spec_version.restype = i32
@@ -109,6 +111,19 @@ def _load():
     lib.spec_compress_prompts.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp, vp]
     lib.spec_assemble_next.restype = i32
     lib.spec_assemble_next.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp]
+    lib.spec_kv_reserve_workspace_bytes.restype = sz
+    lib.spec_kv_reserve_workspace_bytes.argtypes = [i32]
+    lib.spec_kv_reserve.restype = i32
+    lib.spec_kv_reserve.argtypes = [vp, i32, i32, vp, vp, vp, i32, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.spec_kv_quantize.restype = i32
+    lib.spec_kv_quantize.argtypes = [vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, vp]
+    lib.spec_kv_dequantize.restype = i32
+    lib.spec_kv_dequantize.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i64, i32, i32, i32, i32, i32, vp, vp]
+    lib.spec_verify_attn_quantized_workspace_bytes.restype = sz
+    lib.spec_verify_attn_quantized_workspace_bytes.argtypes = [i32] * 7
+    lib.spec_verify_attn_quantized.restype = i32
+    lib.spec_verify_attn_quantized.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp,
+                                               i32, i32, i32, i32, i32, i32, i32, i32, i32, f32, vp, vp, sz, vp]
     lib.spec_probe_read.restype = i32
     lib.spec_probe_read.argtypes = [vp, sz, vp, vp]
     lib.spec_probe_read_pages.restype = i32
@@ -395,6 +410,80 @@ def spec_kv_commit_tree(k_cache, v_cache, page_table, seq_lens, qo_indptr, accep
         _ptr(path, torch.int32), path.shape[1] - 1, _ptr(free_list, torch.int32), free_list.shape[0],
         _ptr(free_count, torch.int32), B, Hkv, D, P, _ptr(status_flags, torch.int32), _stream()))
 
+
+# element types of a cache in 8 bits
+KV_TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
+
+def _cache_pair(k_cache, v_cache, k_scale, v_scale):
+    """(num_pages, Hkv, page size, D, type) of an 8-bit cache."""
+    num_pages, Hkv, P, D = k_cache.shape
+    assert k_cache.dtype in KV_TYPES and v_cache.shape == k_cache.shape, (k_cache.dtype, k_cache.shape, v_cache.shape)
+    assert tuple(k_scale.shape) == (num_pages, Hkv) and tuple(v_scale.shape) == (num_pages, Hkv), (k_scale.shape, v_scale.shape)
+    return num_pages, Hkv, P, D, KV_TYPES[k_cache.dtype]
+
+
+def _row_pair(k, v, Hkv, D):
+    """(rows, stride between rows) of K/V rows [M, Hkv, D] bf16 that are contiguous inside a row and lie equally far apart."""
+    M = k.shape[0]
+    assert tuple(k.shape) == (M, Hkv, D) and v.shape == k.shape, (k.shape, v.shape)
+    assert k.is_cuda and v.is_cuda and k.dtype == v.dtype == torch.bfloat16, (k.dtype, v.dtype)
+    stride = k.stride(0) if M > 1 else Hkv * D
+    for t in (k, v):
+        assert t.stride(2) == 1 and (Hkv == 1 or t.stride(1) == D) and (M <= 1 or t.stride(0) == stride), (k.stride(), v.stride())
+    return M, stride
+
+
+def spec_kv_reserve_workspace_bytes(B):
+    return int(_lib.spec_kv_reserve_workspace_bytes(int(B)))
+
+
+def spec_kv_reserve(page_table, num_pages, seq_lens, qo_indptr, free_list, free_count, slot_map, page_size, status_flags, workspace):
+    B = seq_lens.shape[0]
+    assert page_table.shape[0] == B and qo_indptr.shape[0] == B + 1
+    _check(_lib.spec_kv_reserve(
+        _ptr(page_table, torch.int32), page_table.shape[1], int(num_pages), _ptr(seq_lens, torch.int32), _ptr(qo_indptr, torch.int32),
+        _ptr(free_list, torch.int32), free_list.shape[0], _ptr(free_count, torch.int32), _ptr(slot_map, torch.int32), B, slot_map.shape[0],
+        int(page_size), _ptr(status_flags, torch.int32),
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()))
+
+
+def spec_kv_quantize(k, v, slot_map, k_cache, v_cache, k_scale, v_scale, status_flags):
+    """k, v [M, Hkv, D] bf16, rows possibly strided (slices of a projection's output); k_cache, v_cache float8_e4m3fn or int8."""
+    num_pages, Hkv, P, D, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
+    M, stride = _row_pair(k, v, Hkv, D)
+    assert slot_map.shape[0] == M
+    _check(_lib.spec_kv_quantize(
+        k.data_ptr(), v.data_ptr(), stride, _ptr(slot_map, torch.int32), _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32),
+        _ptr(v_scale, torch.float32), num_pages, M, Hkv, D, P, kv_type, _ptr(status_flags, torch.int32), _stream()))
+
+
+def spec_kv_dequantize(k_cache, v_cache, k_scale, v_scale, slot_map, k, v, status_flags):
+    """k, v [M, Hkv, D] bf16 as for spec_kv_quantize."""
+    num_pages, Hkv, P, D, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
+    M, stride = _row_pair(k, v, Hkv, D)
+    assert slot_map.shape[0] == M
+    _check(_lib.spec_kv_dequantize(
+        _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), num_pages, _ptr(slot_map, torch.int32),
+        k.data_ptr(), v.data_ptr(), stride, M, Hkv, D, P, kv_type, _ptr(status_flags, torch.int32), _stream()))
+
+
+def spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, max_q_len):
+    return int(_lib.spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, max_q_len))
+
+
+def spec_verify_attn_quantized(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, out, lse, max_kv_len, max_q_len, scale,
+                               status_flags, workspace):
+    M, Hq, D = q.shape
+    num_pages, Hkv, P, Dk, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
+    B = seq_lens.shape[0]
+    assert Dk == D and page_table.shape[0] == B and qo_indptr.shape[0] == B + 1 and out.shape == q.shape and (lse is None or tuple(lse.shape) == (M, Hq))
+    _check(_lib.spec_verify_attn_quantized(
+        _ptr(q, torch.bfloat16), _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32),
+        _ptr(page_table, torch.int32), page_table.shape[1], num_pages, _ptr(seq_lens, torch.int32),
+        _ptr(qo_indptr, torch.int32), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
+        B, M, Hq, Hkv, D, P, kv_type, int(max_kv_len), int(max_q_len), float(scale), _ptr(status_flags, torch.int32),
+        _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()))
 
 
 def spec_probe_read(src, sink):

@@ -16,7 +16,7 @@ LIB = os.path.join(HERE, "libspecverify.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 # (the slowest to compile first)
 SOURCES = ["lm_head_rowmajor.hip", "lm_head_rowmajor_stream.hip", "lm_head_mfma_summary.hip", "lm_head_tile.hip", "lm_head_mfma_buffer.hip", "lm_head_mfma_global.hip", "lm_head_mfma_stream.hip",
-           "verify_attn.hip", "lm_head_mfma.hip", "lm_head_packed.hip", "lm_head.hip", "api.hip", "accept.hip", "kv_commit.hip", "assemble_next.hip", "draft_side.hip", "probes.hip"]
+           "verify_attn.hip", "verify_attn_quant.hip", "lm_head_mfma.hip", "lm_head_packed.hip", "lm_head.hip", "api.hip", "accept.hip", "kv_commit.hip", "kv_reserve.hip", "kv_quant.hip", "assemble_next.hip", "draft_side.hip", "probes.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

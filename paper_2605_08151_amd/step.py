@@ -10,7 +10,7 @@ from . import binding as sv
 
 
 class VerifyStep:
-    def __init__(self, B, M, Hq, Hkv, D, H, V, gamma_max, max_kv_len, device="cuda"):
+    def __init__(self, B, M, Hq, Hkv, D, H, V, gamma_max, max_kv_len, device="cuda", quantized_cache=False):
         self.B, self.M, self.Hq, self.Hkv, self.D, self.H, self.V = B, M, Hq, Hkv, D, H, V
         self.gamma_max, self.max_kv_len = gamma_max, max_kv_len
         dev = torch.device(device)
@@ -39,6 +39,28 @@ class VerifyStep:
         self.sblk_max = torch.empty((M, max(1, self.sblocks)), dtype=torch.float32, device=dev)
         self.sblk_sum = torch.empty((M, max(1, self.sblocks)), dtype=torch.float32, device=dev)
         self.sblk_span = torch.empty((max(1, self.sblocks), 2), dtype=torch.int32, device=dev)
+
+        # pages and slots of the step's rows, and attention over a cache in 8 bits
+        self.slot_map = torch.full((M,), -1, dtype=torch.int32, device=dev)
+        self.reserve_ws = torch.empty(max(256, sv.spec_kv_reserve_workspace_bytes(B)), dtype=torch.uint8, device=dev)
+        if quantized_cache:
+            self.quantized_ws = torch.empty(max(256, sv.spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, gamma_max + 1)),
+                                            dtype=torch.uint8, device=dev)
+
+    def reserve(self, page_table, num_pages, seq_lens, qo_indptr, free_list, free_count, page_size=16):
+        """Pages for the step's rows; their slots, for whoever writes the K/V (quantize() for a cache in 8 bits)."""
+        sv.spec_kv_reserve(page_table, num_pages, seq_lens, qo_indptr, free_list, free_count, self.slot_map, page_size, self.status, self.reserve_ws)
+        return self.slot_map
+
+    def quantize(self, k, v, k_cache, v_cache, k_scale, v_scale):
+        """The step's K/V rows into the slots that reserve() found."""
+        sv.spec_kv_quantize(k, v, self.slot_map, k_cache, v_cache, k_scale, v_scale, self.status)
+
+    def attn_quantized(self, q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, scale, want_lse=True):
+        """attn() over a cache in 8 bits (VerifyStep(..., quantized_cache=True))."""
+        sv.spec_verify_attn_quantized(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, self.attn_out,
+                                      self.lse if want_lse else None, self.max_kv_len, self.gamma_max + 1, scale, self.status, self.quantized_ws)
+        return self.attn_out
 
     def lm_head_packed_summary(self, hidden, Wp, temperature, qo_indptr):
         sv.spec_lm_head_packed_summary(hidden, Wp, self.logits, temperature, qo_indptr, self.sblk_max, self.sblk_sum, self.sblk_span)
