@@ -8,7 +8,7 @@
 // HBM-bound: 256 bytes of K + V per key and kv head.  As in verify_attn.hip a workgroup streams one chunk of one request's keys for one kv head, a wave owns 32 keys
 // (two pages) of every step, scores are computed transposed (S^T = K Q^T, so that exp(S^T) is the B operand of O^T += V^T P^T), chunks leave fp32 partials and a second kernel
 // merges them.  Unlike there nothing of K and V goes through LDS: the order of d in a score is free, and with half the bytes a lane's operands are what it loads itself:
-//   K: lane (l16, g) holds key l16, bytes 64 i + 16 g .. + 15 (i = 0, 1): MFMA 2 i + h contracts d = 64 i + 16 g + 8 h .. + 7, and Q is laid out alike;
+//   K: lane (l16, g) holds key l16, d = 32 g .. + 31: MFMA s contracts d = 32 g + 8 s .. + 7, and Q is laid out alike;
 //   V: lane (l16, g) holds d = 8 l16 .. + 7 of keys 4 g .. 4 g + 3: byte t of the four rows, paired by v_perm, converts to the A operand of output tile t, whose rows are
 //      d = 8 m + t.  A lane then ends with d = 32 g .. 32 g + 31 of its query row.
 // The next step's K is requested as soon as this one's is converted, its V likewise.
@@ -27,7 +27,9 @@ extern Tunable g_attn_plan_waves;
 constexpr int kQuantWaves = 4;               // waves per workgroup
 constexpr int kQuantStep = kQuantWaves * 32; // keys per workgroup step
 constexpr int kQuantTiles = 3;               // row tiles (16 query rows) a workgroup takes at most
+constexpr int kQuantStages = 2;              // steps of a wave that are in flight
 constexpr int kQuantPageBytes = kP * kD;
+constexpr int kQuantStageBytes = 4 * kQuantPageBytes;    // two pages of K, two of V
 
 struct QuantAttnParams {
     AttnParams a;                            // (k_cache, v_cache: not used)
@@ -36,7 +38,10 @@ struct QuantAttnParams {
     const float* k_scale;                    // [num_pages, Hkv]
     const float* v_scale;
     int page_slots;                          // 4-byte slots of a chunk's page ids in LDS
+    uint32_t q_sign;                         // flips the sign of two query elements: a negative softmax scale (a.scale_log2e is its magnitude)
 };
+
+constexpr int kQuantWgsPerCu = 2;            // 64 KB of pages in flight each
 
 // two cached elements (bytes 2 HI, 2 HI + 1 of a word) as bf16
 template <int TYPE, bool HI>
@@ -46,23 +51,28 @@ __device__ inline uint32_t bf16_pair(uint32_t raw)
     else return pack_bf16x2((float)(int8_t)(raw >> (HI ? 16 : 0)), (float)(int8_t)(raw >> (HI ? 24 : 8)));
 }
 
+// (The empty statement keeps the words whole up to here: the compiler otherwise takes them apart where they are loaded, a step earlier, into a register per byte.)
 template <int TYPE>
 __device__ inline bf16x8 bf16_oct(uint32_t a, uint32_t b)
 {
+    asm("" : "+v"(a), "+v"(b));
     const u32x4 w = {bf16_pair<TYPE, false>(a), bf16_pair<TYPE, true>(a), bf16_pair<TYPE, false>(b), bf16_pair<TYPE, true>(b)};
     return __builtin_bit_cast(bf16x8, w);
 }
 
 // NR: row tiles per workgroup; FINAL: no request is split, the workgroup normalises and writes bf16 itself.
 template <int NR, int TYPE, bool FINAL>
-__global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(QuantAttnParams qp)
+__global__ __launch_bounds__(kQuantWaves * 64, kQuantWgsPerCu) void verify_attn_quant_kernel(QuantAttnParams qp)
 {
     constexpr int NW = kQuantWaves, kThreads = NW * 64;
-    constexpr int kSliceD = NR == 1 ? kD : (NR == 2 ? kD / 2 : kD / 4), kSlices = kD / kSliceD, kChunks = kSliceD / 4;
+    constexpr int kWaveBytes = kQuantStages * kQuantStageBytes;
+    constexpr int kSlices = (NR * 16 * kD * 4 + kWaveBytes - 1) / kWaveBytes, kSliceD = kD / kSlices, kChunks = kSliceD / 4;
+    static_assert(kD % kSlices == 0 && kSliceD % 32 == 0 && NR * 16 * kSliceD * 4 <= kWaveBytes, "a wave's slice of O fits its buffers");
     const AttnParams& p = qp.a;
-    __shared__ __attribute__((aligned(16))) float sO[NW * NR * 16 * kSliceD];
-    __shared__ float s_m[NW * NR * 16], s_l[NW * NR * 16];
-    extern __shared__ __attribute__((aligned(16))) int32_t sPT[];
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    u32x4* sQ = reinterpret_cast<u32x4*>(smem + NW * kWaveBytes);                        // [NR * 4][64], not with one row tile
+    float* sScale = reinterpret_cast<float*>(sQ + (NR == 1 ? 0 : NR * 4 * 64));          // scales of the chunk's pages: K's, then V's
+    int32_t* sPT = reinterpret_cast<int32_t*>(sScale + 2 * qp.page_slots);               // ... and their ids
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -109,59 +119,58 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
         if (page < 0 || page >= p.num_pages) { page = 0; bad_page = 1; }
         sPT[pg] = page;
     }
-    bf16x8 qf[NR][4];
+    // Q fragments: one row tile stays in registers, more are read again from LDS, where wave w leaves fragment w of every tile
+    bf16x8 qf[4];
+    auto load_q = [&](int rt, int s) {
+        const int r = rt * 16 + l16, j = (first_row + r) / G, gq = first_row + r - j * G;
+        u32x4 x = {0, 0, 0, 0};
+        if (r < R) x = *reinterpret_cast<const u32x4*>(p.q + ((size_t)(r0 + j) * p.Hq + kvh * G + gq) * kD + g * 32 + s * 8);
+        return x ^ qp.q_sign;
+    };
+    if constexpr (NR == 1) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) qf[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
+    } else {
+#pragma unroll
+        for (int rt = 0; rt < NR; ++rt) sQ[(rt * 4 + wave) * 64 + lane] = load_q(rt, wave);
+    }
     int limit[NR];                    // row sees key positions t < limit
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
-        const int r = rt * 16 + l16, j = (first_row + r) / G, gq = first_row + r - j * G;
-        limit[rt] = r < R ? min(c + j + 1, kend) : 0;
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            u32x4 x = {0, 0, 0, 0};
-            if (r < R) x = *reinterpret_cast<const u32x4*>(p.q + ((size_t)(r0 + j) * p.Hq + kvh * G + gq) * kD + (s >> 1) * 64 + g * 16 + (s & 1) * 8);
-            qf[rt][s] = __builtin_bit_cast(bf16x8, x);
-        }
+        const int r = rt * 16 + l16;
+        limit[rt] = r < R ? min(c + (first_row + r) / G + 1, kend) : 0;
     }
     __syncthreads();
 
-    // this wave's two pages of a step; places past the range are read from page 0 and masked
-    u32x4 kraw[2][2];
-    u32x2 vraw[2][4];
-    float scales;                     // lane & 1: which page, lane & 2: K or V
-    const uint32_t koff = (uint32_t)(l16 * kD + g * 16), voff = (uint32_t)(g * 4 * kD + l16 * 8);
-    struct StepPages { int a, b; };
-    auto step_pages = [&](int wbase) {
-        StepPages r;
-        r.a = wbase < kend ? __builtin_amdgcn_readfirstlane(sPT[(wbase - kbeg) / kP]) : 0;
-        r.b = wbase + kP < kend ? __builtin_amdgcn_readfirstlane(sPT[(wbase - kbeg) / kP + 1]) : 0;
-        return r;
-    };
-    auto load_k = [&](StepPages pages) {
+    // This wave's two pages of a step, HBM -> LDS: 2 direct loads of 1 KB per page; places past the range are read from page 0 and masked.  16-byte chunk ch of K's row
+    // (key) r is stored at position ch ^ (r & 7), so that 8 lanes that read the same chunk of 8 rows meet no bank twice; V stays as it is.
+    unsigned char* ring = smem + wave * kWaveBytes;
+    const uint32_t koff = (uint32_t)((lane >> 3) * kD + (((lane & 7) ^ (lane >> 3)) << 4)), voff = (uint32_t)lane * 16;
+    auto issue = [&](int wbase, int stage) {
+        const int a = __builtin_amdgcn_readfirstlane(sPT[(wbase - kbeg) / kP]);
+        const int b = wbase + kP < kend ? __builtin_amdgcn_readfirstlane(sPT[(wbase - kbeg) / kP + 1]) : 0;
+        unsigned char* to = ring + stage * kQuantStageBytes;
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
-            const uint8_t* base = qp.k + ((size_t)(pg ? pages.b : pages.a) * p.Hkv + kvh) * kQuantPageBytes;
+            const size_t at = ((size_t)(pg ? b : a) * p.Hkv + kvh) * kQuantPageBytes;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) kraw[pg][h] = *reinterpret_cast<const u32x4*>(base + koff + h * 64);
+            for (int h = 0; h < 2; ++h) {
+                lds_dma16_off(koff, qp.k + at + h * 1024, to + pg * kQuantPageBytes + h * 1024);
+                lds_dma16_off(voff, qp.v + at + h * 1024, to + (2 + pg) * kQuantPageBytes + h * 1024);
+            }
         }
     };
-    auto load_v = [&](StepPages pages) {
-#pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-            const uint8_t* base = qp.v + ((size_t)(pg ? pages.b : pages.a) * p.Hkv + kvh) * kQuantPageBytes;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) vraw[pg][r] = *reinterpret_cast<const u32x2*>(base + voff + r * kD);
-        }
-    };
-    auto load_scales = [&](StepPages pages) {
-        scales = ((lane & 2) ? qp.v_scale : qp.k_scale)[(size_t)((lane & 1) ? pages.b : pages.a) * p.Hkv + kvh];
-    };
+    constexpr int kLoads = 8;                             // of a stage
     const int wfirst = kbeg + wave * 32;
-    if (wfirst < kend) {
-        const StepPages pages = step_pages(wfirst);
-        load_scales(pages);
-        load_k(pages);
-        load_v(pages);
+#pragma unroll
+    for (int st = 0; st < kQuantStages; ++st)
+        if (wfirst + st * kQuantStep < kend) issue(wfirst + st * kQuantStep, st);
+    // (behind the first pages' requests: a second round trip that flies with them)
+    for (int pg = tid; pg < 2 * qp.page_slots; pg += kThreads) {
+        const int at = pg < qp.page_slots ? pg : pg - qp.page_slots;
+        sScale[pg] = at < npages ? (pg < qp.page_slots ? qp.k_scale : qp.v_scale)[(size_t)sPT[at] * p.Hkv + kvh] : 0.0f;
     }
+    __syncthreads();
 
     f32x4 o[NR][8];
     float m_run[NR], l_run[NR];
@@ -175,19 +184,32 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
 
     auto run_chunk = [&](auto active) {
     constexpr int A = decltype(active)::value;
+    int stage = 0;
     for (int wbase = wfirst; wbase < kend; wbase += kQuantStep) {
-        const bool more = wbase + kQuantStep < kend;
-        StepPages next{0, 0};
-        if (more) next = step_pages(wbase + kQuantStep);
-        float ks[2], vs[2];
+        // this step's pages have landed, the next one's may fly on; once they are in registers, their place is for the step behind that
+        if (wbase + kQuantStep < kend) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kQuantStages - 1)) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        u32x4 kraw[2][2];
+        u32x2 vraw[2][4];
+        const unsigned char* sK = ring + stage * kQuantStageBytes;
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
-            ks[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), pg)) * p.scale_log2e;
-            vs[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), 2 + pg));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) kraw[pg][h] = *reinterpret_cast<const u32x4*>(sK + pg * kQuantPageBytes + l16 * kD + (((2 * g + h) ^ (l16 & 7)) << 4));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) vraw[pg][r] = *reinterpret_cast<const u32x2*>(sK + (2 + pg) * kQuantPageBytes + (4 * g + r) * kD + l16 * 8);
         }
-        if (wbase + kP >= kend) { ks[1] = 0.0f; vs[1] = 0.0f; }      // no second page: its stand-in's scale may be anything
-        if (more) load_scales(next);
-        // ---- S^T = K Q^T ----
+        float ks[2], vs[2];
+        const int at = (wbase - kbeg) / kP;               // (a page that is not there has scales 0)
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) { ks[pg] = sScale[at + pg] * p.scale_log2e; vs[pg] = sScale[qp.page_slots + at + pg]; }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (wbase + kQuantStages * kQuantStep < kend) issue(wbase + kQuantStages * kQuantStep, stage);
+        stage = stage + 1 == kQuantStages ? 0 : stage + 1;
+        // (two row tiles: Q is read again in every step, 32 registers less; three have room for 48)
+        int q_lane = lane;
+        if constexpr (NR == 2) asm volatile("" : "+v"(q_lane));
+        // ---- S^T = K Q^T; sc * ks is a score in the log2 domain ----
         float sc[A][8];
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) {
@@ -199,39 +221,41 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
                 const u32x4 raw = kraw[pg][s >> 1];
                 const bf16x8 kf = (s & 1) ? bf16_oct<TYPE>(raw.z, raw.w) : bf16_oct<TYPE>(raw.x, raw.y);
 #pragma unroll
-                for (int rt = 0; rt < A; ++rt) acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[rt][s], acc[rt], 0, 0, 0);
+                for (int rt = 0; rt < A; ++rt) {
+                    const bf16x8 qx = NR == 1 ? qf[s] : __builtin_bit_cast(bf16x8, sQ[(rt * 4 + s) * 64 + q_lane]);
+                    acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qx, acc[rt], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int rt = 0; rt < A; ++rt)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[rt][pg * 4 + e] = acc[rt][e] * ks[pg];
+                for (int e = 0; e < 4; ++e) sc[rt][pg * 4 + e] = acc[rt][e];
         }
-        if (more) load_k(next);
         const bool need_mask = wbase + 32 > min(c + 1, kend);
-        if (need_mask) {
+        if (need_mask) {                                  // (a scale may be 0: masked scores are scaled ones)
 #pragma unroll
             for (int rt = 0; rt < A; ++rt)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (wbase + (e >> 2) * 16 + g * 4 + (e & 3) >= limit[rt]) sc[rt][e] = kNegBig;          // exp2 of it is 0
+                    sc[rt][e] = wbase + (e >> 2) * 16 + g * 4 + (e & 3) < limit[rt] ? sc[rt][e] * ks[e >> 2] : kNegBig;
+            ks[0] = ks[1] = 1.0f;
         }
+        // The reference maximum moves only when a score exceeds it by more than kMaxSlack (see verify_attn.hip): a lane looks at its own 8 scores, and the four
+        // lanes of a query row agree on a new maximum where one of them asks for it.
         float tmax[A];
-#pragma unroll
-        for (int rt = 0; rt < A; ++rt) {
-            float t = sc[rt][0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) t = fmaxf(t, sc[rt][e]);
-            tmax[rt] = four_rows_max(t);
-        }
-        // the reference maximum moves only when a step's maximum exceeds it by more than kMaxSlack (see verify_attn.hip)
         bool grow = false;
 #pragma unroll
-        for (int rt = 0; rt < A; ++rt) grow |= tmax[rt] > m_run[rt] + kMaxSlack;
+        for (int rt = 0; rt < A; ++rt) {
+            const float a = fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])), b = fmaxf(fmaxf(sc[rt][4], sc[rt][5]), fmaxf(sc[rt][6], sc[rt][7]));
+            tmax[rt] = fmaxf(a * ks[0], b * ks[1]);
+            grow |= tmax[rt] > m_run[rt] + kMaxSlack;
+        }
         if (__any(grow)) {
 #pragma unroll
             for (int rt = 0; rt < A; ++rt)
                 if (__any(tmax[rt] > m_run[rt] + kMaxSlack)) {
-                    const float m_new = fmaxf(m_run[rt], tmax[rt]);
+                    const float m_new = fmaxf(m_run[rt], four_rows_max(tmax[rt]));
                     const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
                     m_run[rt] = m_new;
                     l_run[rt] *= alpha;
@@ -245,7 +269,7 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
             float pr[8], psum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                pr[e] = __builtin_amdgcn_exp2f(sc[rt][e] - m_run[rt]);
+                pr[e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
                 // (a row that has seen nothing at all has m_run == kNegBig)
                 if (need_mask) pr[e] = sc[rt][e] > 0.5f * kNegBig ? pr[e] : 0.0f;
                 psum += pr[e];
@@ -271,11 +295,12 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
             for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
-                    const uint32_t a = w ? vraw[pg][2 * k2].y : vraw[pg][2 * k2].x, b = w ? vraw[pg][2 * k2 + 1].y : vraw[pg][2 * k2 + 1].x;
+                    uint32_t a = w ? vraw[pg][2 * k2].y : vraw[pg][2 * k2].x, b = w ? vraw[pg][2 * k2 + 1].y : vraw[pg][2 * k2 + 1].x;
+                    asm("" : "+v"(a), "+v"(b));
                     pair[pg][k2][2 * w] = __builtin_amdgcn_perm(b, a, 0x05010400u);
                     pair[pg][k2][2 * w + 1] = __builtin_amdgcn_perm(b, a, 0x07030602u);
                 }
-        if (more) load_v(next);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             u32x4 w;
@@ -284,6 +309,7 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
             const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
             for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o[rt][t], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     };
@@ -296,7 +322,10 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
 
     // ---- merge the waves, in slices of d: each leaves its O (16-byte chunk c of a row at position c ^ (row & 7)), maxima and sums; a thread then takes 4
     // consecutive d of a row from all waves ----
-    float* own = sO + wave * NR * 16 * kSliceD;
+    float* s_m = sScale;                                  // [NW][NR * 16] (every wave has read its scales, see the barrier)
+    float* s_l = s_m + NW * NR * 16;
+    float* own = reinterpret_cast<float*>(ring);
+    __syncthreads();
 #pragma unroll
     for (int rt = 0; rt < NR; ++rt) {
         const float l = four_rows_sum(l_run[rt]);
@@ -335,7 +364,7 @@ __global__ __launch_bounds__(kQuantWaves * 64) void verify_attn_quant_kernel(Qua
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float f = __builtin_amdgcn_exp2f(m[w] - mx);
-                num += f * *reinterpret_cast<const f32x4*>(sO + (w * NR * 16 + r) * kSliceD + ((ch ^ (r & 7)) << 2));
+                num += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * kWaveBytes) + r * kSliceD + ((ch ^ (r & 7)) << 2));
                 l += f * s_l[w * NR * 16 + r];
             }
             const int j = (first_row + r) / G, gq = first_row + r - j * G;
@@ -364,7 +393,7 @@ struct QuantPlan {
     size_t hdr_bytes, req_bytes, items_bytes, slots;
 };
 
-constexpr int kQuantMinChunk = 256, kQuantMaxChunk = 8192;
+constexpr int kQuantMinChunk = 256, kQuantMaxChunk = 4096;
 
 static QuantPlan quant_plan(int B, int M, int Hq, int Hkv, int max_kv_len, int max_q_len)
 {
@@ -372,7 +401,7 @@ static QuantPlan quant_plan(int B, int M, int Hq, int Hkv, int max_kv_len, int m
     const int NR = (Hq / Hkv * max_q_len + 15) / 16;
     c.groups = (NR + kQuantTiles - 1) / kQuantTiles;
     c.tiles = (NR + c.groups - 1) / c.groups;
-    const long cus = device_cu_count(), per_cu = 4;
+    const long cus = device_cu_count(), per_cu = kQuantWgsPerCu;
     const int forced = g_attn_chunk_override;
     long target = forced > 0 ? forced : (long)B * Hkv * max_kv_len / (cus * per_cu);
     if (forced <= 0) target = std::min<long>(std::max<long>(target, kQuantMinChunk), 4096);
@@ -396,19 +425,32 @@ static size_t quant_workspace(const QuantPlan& c)
     return (c.list ? c.hdr_bytes + c.req_bytes + c.items_bytes : 0) + round_up(c.slots * kD * 4, 256) + 2 * round_up(c.slots * 4, 256);
 }
 
-template <int NR, int TYPE>
-static void launch_quant_as(const QuantAttnParams& p, dim3 grid, hipStream_t s)
+// LDS: the waves' pages, Q, and the scales and ids of a chunk's pages (where the waves' maxima and sums stand at the end)
+static size_t quant_smem(int NR, int page_slots)
 {
-    const size_t smem = (size_t)p.page_slots * 4;
-    if (p.a.splits == 1) hipLaunchKernelGGL((verify_attn_quant_kernel<NR, TYPE, true>), grid, dim3(kQuantWaves * 64), smem, s, p);
-    else hipLaunchKernelGGL((verify_attn_quant_kernel<NR, TYPE, false>), grid, dim3(kQuantWaves * 64), smem, s, p);
+    return (size_t)kQuantWaves * kQuantStages * kQuantStageBytes + (NR == 1 ? 0 : (size_t)NR * 16 * kD * 2) + std::max<size_t>((size_t)page_slots * 12, (size_t)kQuantWaves * NR * 16 * 8);
+}
+
+template <int NR, int TYPE, bool FINAL>
+static int launch_quant_one(const QuantAttnParams& p, dim3 grid, hipStream_t s)
+{
+    const size_t smem = quant_smem(NR, p.page_slots);
+    static LdsGrantTable granted = {};
+    if (int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(&verify_attn_quant_kernel<NR, TYPE, FINAL>), smem, granted, "spec_verify_attn_quantized")) return rc;
+    hipLaunchKernelGGL((verify_attn_quant_kernel<NR, TYPE, FINAL>), grid, dim3(kQuantWaves * 64), smem, s, p);
+    return SPEC_OK;
+}
+
+template <int NR, int TYPE>
+static int launch_quant_as(const QuantAttnParams& p, dim3 grid, hipStream_t s)
+{
+    return p.a.splits == 1 ? launch_quant_one<NR, TYPE, true>(p, grid, s) : launch_quant_one<NR, TYPE, false>(p, grid, s);
 }
 
 template <int NR>
-static void launch_quant(const QuantAttnParams& p, int kv_type, dim3 grid, hipStream_t s)
+static int launch_quant(const QuantAttnParams& p, int kv_type, dim3 grid, hipStream_t s)
 {
-    if (kv_type == SPEC_KV_E4M3) launch_quant_as<NR, SPEC_KV_E4M3>(p, grid, s);
-    else launch_quant_as<NR, SPEC_KV_INT8>(p, grid, s);
+    return kv_type == SPEC_KV_E4M3 ? launch_quant_as<NR, SPEC_KV_E4M3>(p, grid, s) : launch_quant_as<NR, SPEC_KV_INT8>(p, grid, s);
 }
 
 }  // namespace specv
@@ -461,7 +503,8 @@ extern "C" int spec_verify_attn_quantized(const void* q, const void* k_cache, co
     a.max_pages = max_pages_per_seq; a.num_pages = num_pages; a.Hq = Hq; a.Hkv = Hkv; a.G = G;
     a.M = M; a.max_kv_len = max_kv_len; a.max_q_len = max_q_len; a.B = B;
     a.chunk_target = c.chunk; a.splits = c.splits;
-    a.scale_log2e = scale * 1.4426950408889634f;
+    a.scale_log2e = fabsf(scale) * 1.4426950408889634f;
+    p.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     p.k = (const uint8_t*)k_cache; p.v = (const uint8_t*)v_cache; p.k_scale = k_scale; p.v_scale = v_scale;
     hipStream_t s = (hipStream_t)stream;
     char* parts = (char*)workspace;
@@ -481,16 +524,19 @@ extern "C" int spec_verify_attn_quantized(const void* q, const void* k_cache, co
     a.part_o = (float*)parts;
     a.part_m = (float*)(parts + round_up(c.slots * kD * 4, 256));
     a.part_l = (float*)(parts + round_up(c.slots * kD * 4, 256) + round_up(c.slots * 4, 256));
-    p.page_slots = std::min(a.chunk_target, max_kv_len) / kP + 2;
+    p.page_slots = (std::min(a.chunk_target, max_kv_len) / kP + 3) & ~1;     // a step's second page may lie one behind the chunk's last
     a.turn = piece_turn(Hkv, a.splits);
     a.head_first = grid.x <= 65535;                       // (the second dimension's limit)
     if (a.head_first) grid = dim3(grid.y, grid.x, grid.z);
+    int rc = SPEC_OK;
     switch (c.tiles) {
-        case 1: launch_quant<1>(p, kv_type, grid, s); break;
-        case 2: launch_quant<2>(p, kv_type, grid, s); break;
-        default: launch_quant<3>(p, kv_type, grid, s); break;
+        case 1: rc = launch_quant<1>(p, kv_type, grid, s); break;
+        case 2: rc = launch_quant<2>(p, kv_type, grid, s); break;
+        default: rc = launch_quant<3>(p, kv_type, grid, s); break;
     }
-    if (int rc = check_launch("spec_verify_attn_quantized")) return rc;
+    if (rc != SPEC_OK) return rc;
+    rc = check_launch("spec_verify_attn_quantized");
+    if (rc != SPEC_OK) return rc;
     if (a.splits == 1) return SPEC_OK;
     return launch_attn_merge(a, B, c.list ? (c.target_items + B) / B <= 8 : a.splits <= 16, s);
 }
