@@ -18,7 +18,8 @@
 //   Every chunk writes an unnormalised fp32 partial (O, running max, sum); a second kernel merges the
 //   partials of a row in split order (deterministic) and writes bf16.
 #include "attn_lds.h"
-#include "attn_params.h"
+#include "batch_rules.h"
+#include "common.h"
 #include "kv_stream.h"
 
 #include <algorithm>
@@ -27,10 +28,15 @@
 
 namespace specv {
 
+constexpr int kD = 128;                      // head dimension
+constexpr int kP = 16;                       // tokens per page
 constexpr int kRowBytes = kD * 2;            // one K or V row in LDS (unpadded, swizzled)
 constexpr int kWaveLds = 2 * 32 * kRowBytes; // per wave: 32 K rows + 32 V rows = 16 KB
+constexpr float kNegBig = -1.0e30f;          // "nothing seen yet" running maximum (log2 domain)
+constexpr float kMaxSlack = 6.0f;            // how far a step's maximum may exceed the reference before a rescale
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));    // (rows of the output may start at any element)
 
 // Transposing LDS read.  In every group of 16 lanes, lane r supplies the address of 4 consecutive
 // 16-bit elements M[r][0..3]; lane j receives M[j/4][j%4], M[4 + j/4][j%4], M[8 + j/4][j%4], M[12 + j/4][j%4].
@@ -38,6 +44,39 @@ __device__ inline s16x4 lds_read_tr(const void* lds)
 {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds);
 }
+
+struct AttnParams {
+    const uint16_t* q;
+    const uint16_t* k_cache;
+    const uint16_t* v_cache;
+    const int32_t* page_table;
+    const int32_t* seq_lens;
+    const int32_t* qo_indptr;
+    uint16_t* out;      // [M, Hq, 128] bf16
+    float* lse;         // [M, Hq] or null
+    float* part_o;      // [M*Hq, splits, 128]
+    float* part_m;      // [M*Hq, splits]   running max, log2 domain
+    float* part_l;      // [M*Hq, splits]
+    int32_t* status_flags;
+    // balanced work list written by verify_attn_plan_kernel (all null when requests are split by the fixed
+    // chunk_target instead): hdr = {items, keys per chunk, K/V too large for the memory-side cache}; req[i] = {splits of request i, first partial slot};
+    // items[k] = {request, split, splits of the request, first partial slot}
+    const int32_t* parent;     // tree verification: row-local parent of every candidate row ([M], -1 for a root), or null = chains
+    const int32_t* plan_hdr;
+    const int32_t* plan_req;
+    const int32_t* plan_items;
+    int max_pages, num_pages, Hq, Hkv, G, M, max_kv_len, max_q_len, chunk_target, splits;
+    float scale_log2e;
+    int B;
+    // Workgroups that start together take the heads of one piece: their pages are neighbours in HBM (a page of all heads is one stretch of Hkv * 4 KB), and are
+    // read at about the same time.  Pieces first -> heads first: 128 requests x 8 heads x 2.6k keys 266.7 -> 220.7 us (5.2 -> 6.3 TB/s)
+    int head_first;
+    PieceTurn turn;            // fixed chunks: which piece of its request a place in the grid stands for
+    // Fixed chunks, at most 64 requests, more workgroups than CUs: the requests with the longest contexts go first (see longest_first)
+    int by_length;
+    int page_slots;            // see attn_page_slots
+    float stream_keys;         // committed keys of the batch above which its K/V is too large for the memory-side cache (0: it never is)
+};
 
 // The kernels with STREAM read a chunk's pages by nontemporal loads where kv_stream.h says so: the last wave looks (beside the first one's loads of the
 // chunk's page ids) and leaves the answer in LDS for the others behind the barrier that publishes those.  The work list's kernel knows the batch's total and
@@ -50,6 +89,31 @@ __device__ inline void kv_scan(const AttnParams& p, int i, int page, bool total_
     const bool shared = __any(s.shared);
     const float keys = total_known ? INFINITY : four_rows_sum(row16_sum(s.keys));
     if (threadIdx.x == (NW - 1) * 64) *answer = keys > p.stream_keys && !shared;
+}
+
+__device__ inline bool request_ok(int r0, int n, int c, const AttnParams& p)
+{
+    return n >= 1 && n <= p.max_q_len && r0 >= 0 && r0 + n <= p.M && c >= 0 && c + n <= p.max_kv_len;
+}
+
+// Request number `rank` in the order of committed keys, longest first (ties: request order), and its metadata.  A lane per request (at most 64); one memory round trip,
+// like reading the request of the grid's own order.  Workgroups start in grid order, one per CU, so that the last ones decide when the call ends: 64 requests of
+// 1-4k keys x 8 heads, 5 rows 114.0 -> 105.7 us; 16 trees of 0.5-4k keys x 8 heads 40.0 -> 38.3.
+struct RequestRef { int i, r0, n, c; };
+
+__device__ inline RequestRef longest_first(const AttnParams& p, int rank)
+{
+    const int lane = threadIdx.x & 63;
+    int c = 0, q0 = 0, q1 = 0;
+    if (lane < p.B) { c = p.seq_lens[lane]; q0 = p.qo_indptr[lane]; q1 = p.qo_indptr[lane + 1]; }
+    // lanes past the batch: below all others
+    const uint32_t key = (uint32_t)min(max(c, 0), (1 << 25) - 1) * 64u + (uint32_t)(63 - lane);
+    int above = 0;
+#pragma unroll
+    for (int k = 0; k < 64; ++k) above += (uint32_t)__builtin_amdgcn_readlane((int)key, k) > key;
+    const int i = __ffsll((long long)__ballot(above == rank)) - 1;
+    const int r0 = __builtin_amdgcn_readlane(q0, i);
+    return {i, r0, __builtin_amdgcn_readlane(q1, i) - r0, __builtin_amdgcn_readlane(c, i)};
 }
 
 // NR: 16-row query tiles per (request, kv head); NW: waves per workgroup (each owns 32 keys of a step);
@@ -1002,22 +1066,6 @@ __global__ __launch_bounds__(256) void verify_attn_combine_rows_kernel(AttnParam
     if (p.lse && (tid & 31) == 0) p.lse[(size_t)row * p.Hq + hq] = (mx + log2f(den)) * 0.6931471805599453f;
 }
 
-int launch_attn_plan(const AttnParams& p, int B, int target_items, int step_keys, int min_chunk, int max_chunk, int max_items, int32_t* hdr, int32_t* req,
-                     int32_t* items, hipStream_t s)
-{
-    hipLaunchKernelGGL(verify_attn_plan_kernel, dim3(1), dim3((B + 63) / 64 * 64), 0, s, p, B, target_items, step_keys, min_chunk, max_chunk, max_items, hdr,
-                       req, items);
-    return check_launch("spec_verify_attn (plan)");
-}
-
-// few: few pieces per request
-int launch_attn_merge(const AttnParams& p, int B, bool few, hipStream_t s)
-{
-    if (few) hipLaunchKernelGGL(verify_attn_combine_rows_kernel, dim3(p.M, (p.Hq + 7) / 8), dim3(256), 0, s, p, B);
-    else hipLaunchKernelGGL(verify_attn_combine_kernel, dim3(p.M, p.Hq), dim3(256), 0, s, p, B);
-    return check_launch("spec_verify_attn (combine)");
-}
-
 Tunable g_attn_chunk_override{0};
 
 // Keys per kv split.  A split costs a prologue (Q to LDS), an epilogue (cross-wave merge) and a partial
@@ -1258,7 +1306,9 @@ extern "C" int spec_verify_attn_tree(const void* q, const void* k_cache, const v
         p.part_o = (float*)parts;
         p.part_m = (float*)(parts + round_up(pc.slots * kD * 4, 256));
         p.part_l = (float*)(parts + round_up(pc.slots * kD * 4, 256) + round_up(pc.slots * 4, 256));
-        int prc = launch_attn_plan(p, B, pc.target_items, pc.step_keys, kPlanMinChunk, kPlanMaxChunk, pc.max_items, hdr, req, items, s);
+        hipLaunchKernelGGL(verify_attn_plan_kernel, dim3(1), dim3((B + 63) / 64 * 64), 0, s, p, B, pc.target_items, pc.step_keys,
+                           kPlanMinChunk, kPlanMaxChunk, pc.max_items, hdr, req, items);
+        int prc = check_launch("spec_verify_attn (plan)");
         if (prc != SPEC_OK) return prc;
         p.plan_hdr = hdr; p.plan_req = req; p.plan_items = items;
         p.chunk_target = kPlanMaxChunk;                   // sizes the page-id staging area in LDS
@@ -1294,5 +1344,7 @@ extern "C" int spec_verify_attn_tree(const void* q, const void* k_cache, const v
     if (p.splits == 1) return SPEC_OK;                    // the main kernel wrote the output itself
     // few pieces per request (typical count in work-list mode: items per request): one workgroup per row
     const bool few = pc.on ? (pc.target_items + B) / B <= 8 : p.splits <= 16;
-    return launch_attn_merge(p, B, few, s);
+    if (few) hipLaunchKernelGGL(verify_attn_combine_rows_kernel, dim3(M, (Hq + 7) / 8), dim3(256), 0, s, p, B);
+    else hipLaunchKernelGGL(verify_attn_combine_kernel, dim3(M, Hq), dim3(256), 0, s, p, B);
+    return check_launch("spec_verify_attn (combine)");
 }
