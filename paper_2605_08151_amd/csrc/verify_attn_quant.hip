@@ -16,6 +16,7 @@
 //   V: lane (l16, g) holds d = 8 l16 .. + 7 of keys 4 g .. 4 g + 3: byte t of the four rows, paired by v_perm, converts to the A operand of output tile t, whose rows are
 //      d = 8 m + t.  A lane then ends with d = 32 g .. 32 g + 31 of its query row.
 #include "common.h"
+#include "kv_stream.h"
 
 #include <algorithm>
 #include <cmath>
@@ -36,10 +37,12 @@ constexpr int kQuantTiles = 3;               // row tiles (16 query rows) at onc
 constexpr int kQuantStages = 2;              // steps of a wave that are in flight
 constexpr int kQuantWgsPerCu = 2;            // 64 KB of pages each
 constexpr int kQuantListed = 1024;           // requests whose ranges a workgroup finds (four per thread)
+constexpr int kQuantOrdered = kQuantThreads;             // whole requests are taken longest first up to so many
 constexpr int kQuantPageBytes = kP * kD;
 constexpr int kQuantStageBytes = 4 * kQuantPageBytes;    // two pages of K, two of V
 constexpr int kQuantWaveBytes = kQuantStages * kQuantStageBytes;
 constexpr float kNegBig = -1.0e30f;          // "nothing seen yet" running maximum (log2 domain)
+constexpr float kMasked = -2.0e30f;          // a masked score: 0 in the exponential below every maximum
 constexpr float kMaxSlack = 6.0f;            // how far a score may exceed the reference before a rescale
 
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));    // (rows of the output may start at any element)
@@ -65,16 +68,20 @@ struct QuantAttnParams {
     int max_pages, num_pages, Hq, Hkv, G, M, B, max_kv_len, max_q_len;
     int ranges;              // 0: a workgroup takes a whole request
     int min_work;            // of a range, and at least the work of one step of any request
+    uint32_t g_magic;        // r / G = r * g_magic >> 16 for r < 256
+    int by_length;           // whole requests: the longest first
     int groups;              // whole requests: row groups are workgroups of their own (1: the workgroup takes them all)
     float scale_log2e;       // >= 0
+    float stream_keys;       // committed keys of the batch above which its pages are too large for the memory-side cache
     uint32_t q_sign;         // flips the sign of two query elements: a negative softmax scale
 };
 
 // two cached elements (bytes 2 HI, 2 HI + 1 of a word) as bf16
+// (e4m3: times a power of two)
 template <int TYPE, bool HI>
-__device__ inline uint32_t bf16_pair(uint32_t raw)
+__device__ inline uint32_t bf16_pair(uint32_t raw, float power = 1.0f)
 {
-    if constexpr (TYPE == SPEC_KV_E4M3) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw, 1.0f, HI));
+    if constexpr (TYPE == SPEC_KV_E4M3) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw, power, HI));
     else return pack_bf16x2((float)(int8_t)(raw >> (HI ? 16 : 0)), (float)(int8_t)(raw >> (HI ? 24 : 8)));
 }
 
@@ -100,29 +107,50 @@ __host__ __device__ constexpr int quant_step_work(int rows)
     return (tiles + kQuantTiles - 1) / kQuantTiles * 4 + tiles;
 }
 
+// ... and of a piece besides its steps: its first pages' round trip, the merge of its waves
+__host__ __device__ constexpr int quant_piece_work(int rows) { return ((rows + 15) / 16 + kQuantTiles - 1) / kQuantTiles * 20; }
+
 // One piece: keys kbeg .. kend (kbeg a multiple of 128) of request i for one kv head.
 struct QuantPiece { int i, r0, n, c, kbeg, kend; bool whole; size_t slot; };
 
 // A request's first row, rows and committed tokens, the same in every lane by construction: control flow and addresses that depend on them stay scalar.
 struct QuantRequest { int r0, n, c; };
 
+// (read through the scalar cache: a vector load would be waited for together with the pages in flight behind it)
+__device__ inline int scalar_load(const int32_t* x, int i)
+{
+    return ((const __attribute__((address_space(4))) int32_t*)reinterpret_cast<uint64_t>(x))[i];
+}
+
 __device__ inline QuantRequest quant_request(const QuantAttnParams& p, int i)
 {
-    const int r0 = __builtin_amdgcn_readfirstlane(p.qo_indptr[i]), end = __builtin_amdgcn_readfirstlane(p.qo_indptr[i + 1]);
-    return {r0, end - r0, __builtin_amdgcn_readfirstlane(p.seq_lens[i])};
+    const int r0 = scalar_load(p.qo_indptr, i);
+    return {r0, scalar_load(p.qo_indptr, i + 1) - r0, scalar_load(p.seq_lens, i)};
+}
+
+// An address that is the same in every lane, in scalar registers whatever the compiler makes of what it is computed from.  The s_nop is the distance that a load written
+// in assembly needs from a vector instruction that writes its scalar base.
+__device__ inline const uint8_t* scalar_address(const uint8_t* x)
+{
+    const uint64_t bits = reinterpret_cast<uint64_t>(x);
+    uint64_t at = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(bits >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)bits);
+    asm volatile("s_nop 4" : "+s"(at));
+    return reinterpret_cast<const uint8_t*>(at);
 }
 
 // NR: row tiles at once.
 template <int NR, int TYPE>
 struct QuantKernel {
     static constexpr int NW = kQuantWaves;
-    static constexpr int kSlices = (NR * 16 * kD * 4 + kQuantWaveBytes - 1) / kQuantWaveBytes, kSliceD = kD / kSlices, kChunks = kSliceD / 4;
-    static_assert(kD % kSlices == 0 && kSliceD % 32 == 0 && NR * 16 * kSliceD * 4 <= kQuantWaveBytes, "a wave's slice of O fits its buffers");
-    static_assert(kQuantStages == 2, "the waits count the loads of one younger step");
+    static constexpr int kTileBytes = 16 * kD * 4;        // a row tile of O
+    static_assert(kQuantStages == 2 && kTileBytes <= kQuantStageBytes, "the waits count the loads of one younger step; the merge has the place of the second");
     // LDS: the waves' pages, Q, the waves' maxima and sums
     static constexpr size_t kQAt = NW * kQuantWaveBytes, kMlAt = kQAt + (NR == 1 ? 0 : NR * 4 * 64 * 16), kBytes = kMlAt + 2 * NW * NR * 16 * 4;
 
-    static __device__ __forceinline__ void piece(const QuantAttnParams& p, unsigned char* smem, const QuantPiece& u, int kvh, int group)
+    // Pieces one behind the other, `first` and then what next(piece, group) makes of the last one.  While a piece is computed the page ids of the next one are fetched; its
+    // scales, queries and first pages fly while the waves' parts of this one are merged.
+    template <typename Next>
+    static __device__ __forceinline__ void run(const QuantAttnParams& p, unsigned char* smem, int kvh, QuantPiece u, int group, Next next)
     {
         const int tid = threadIdx.x, lane = tid & 63;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -130,304 +158,372 @@ struct QuantKernel {
         u32x4* sQ = reinterpret_cast<u32x4*>(smem + kQAt);                             // [NR * 4][64], not with one row tile
         float* s_m = reinterpret_cast<float*>(smem + kMlAt);                           // [NW][NR * 16]
         float* s_l = s_m + NW * NR * 16;
-        const int G = p.G, first_row = group * kQuantTiles * 16, R = min(G * u.n - first_row, NR * 16);
-        const int c = u.c, kend = u.kend;
+        unsigned char* ring = smem + wave * kQuantWaveBytes;
+        int bad_page = 0;
 
         // ---- page ids and scales of this wave's steps, 32 steps at a time: lane l holds page l % 2 of step l / 2 (page 0 stands in for a bad id, which is flagged,
-        // and with scales 0 for what lies behind the piece) ----
-        const int32_t* pt = p.page_table + (size_t)u.i * p.max_pages + (u.kbeg / kP);
-        const int npages = (kend - u.kbeg + kP - 1) / kP;
-        int ids = 0, bad_page = 0;
-        float ksc = 0.0f, vsc = 0.0f;
-        auto load_ids = [&](int step) {
-            const int pg = (step + (lane >> 1)) * (kQuantStep / kP) + 2 * wave + (lane & 1);
-            ids = 0;
-            if (pg < npages) {
-                ids = pt[pg];
-                if (ids < 0 || ids >= p.num_pages) { ids = 0; bad_page = 1; }
+        // and with scales 0 for what lies behind the piece).  K's scale is that of a score; V's is a power of two, which the conversion of e4m3 applies, and the rest, a
+        // factor of the probabilities that is 1 for the scales that spec_kv_quantize sets ----
+        struct Pages { int id; float ks, vm; uint32_t ve; };
+        auto page_at = [&](int step) { return (step + (lane >> 1)) * (kQuantStep / kP) + 2 * wave + (lane & 1); };
+        auto load_ids = [&](const QuantPiece& x, int step) {
+            const int pg = page_at(step);
+            int id = 0;
+            if (pg * kP < x.kend - x.kbeg) {
+                id = p.page_table[(size_t)x.i * p.max_pages + x.kbeg / kP + pg];
+                if (id < 0 || id >= p.num_pages) { id = 0; bad_page = 1; }
             }
+            return id;
         };
-        auto load_scales = [&](int step) {
-            const int pg = (step + (lane >> 1)) * (kQuantStep / kP) + 2 * wave + (lane & 1);
-            ksc = vsc = 0.0f;
-            if (pg < npages) {
-                ksc = p.k_scale[(size_t)ids * p.Hkv + kvh];
-                vsc = p.v_scale[(size_t)ids * p.Hkv + kvh];
+        auto load_scales = [&](const QuantPiece& x, int step, int id) {
+            Pages r{id, 0.0f, 0.0f, 0x3F800000u};
+            if (page_at(step) * kP < x.kend - x.kbeg) {
+                r.ks = p.k_scale[(size_t)id * p.Hkv + kvh] * p.scale_log2e;
+                r.vm = p.v_scale[(size_t)id * p.Hkv + kvh];
+                if constexpr (TYPE == SPEC_KV_E4M3) {
+                    const uint32_t bits = __builtin_bit_cast(uint32_t, r.vm), power = bits & 0x7F800000u;
+                    r.ve = max(power, 0x00800000u);       // (0 and subnormal numbers: 2^-126)
+                    r.vm = power ? __builtin_bit_cast(float, (bits & 0x807FFFFFu) | 0x3F800000u) : r.vm * 0x1p126f;
+                }
             }
+            return r;
         };
-        load_ids(0);
-        // Q fragments: one row tile stays in registers, more are read again from LDS, where wave w leaves fragment w of every tile
-        bf16x8 qf[4];
-        auto load_q = [&](int rt, int s) {
-            const int r = rt * 16 + l16, j = (first_row + r) / G, gq = first_row + r - j * G;
-            u32x4 x = {0, 0, 0, 0};
-            if (r < R) x = *reinterpret_cast<const u32x4*>(p.q + ((size_t)(u.r0 + j) * p.Hq + kvh * G + gq) * kD + g * 32 + s * 8);
-            return x ^ p.q_sign;
+        // Whether the pages of a piece are read by nontemporal loads (kv_stream.h): every wave looks at a quarter of the up to 64 requests around its own.  A request with more
+        // than kQuantTiles row tiles takes its keys again: ordinary loads but for the last time (256 mixed requests 133 -> 120 us).
+        struct Look { float keys; bool shared; };
+        auto look = [&](const QuantPiece& x) {
+            if (lane >= kKvScanRequests / 4) return Look{0.0f, false};
+            const KvScan s = kv_scan_lane(p.seq_lens, p.page_table, p.max_pages, p.B, p.max_kv_len, x.i, x.kbeg / kP, 4 * lane);
+            return Look{s.keys, s.shared};
         };
-        if constexpr (NR == 1) {
+        auto streams = [&](const QuantPiece& x, int grp, Look l) {
+            const int large = __builtin_amdgcn_readfirstlane(row16_sum(l.keys) > p.stream_keys);           // (lanes 0 .. 15)
+            return (grp + 1) * kQuantTiles * 16 >= p.G * x.n && large && !__any(l.shared);
+        };
+        // Q: one row tile stays in registers, of more tiles wave w takes fragment w of each to LDS
+        constexpr int kQ = NR == 1 ? 4 : NR;
+        struct Query { u32x4 x[kQ]; };
+        auto load_q = [&](const QuantPiece& x, int grp) {
+            Query r;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) qf[s] = __builtin_bit_cast(bf16x8, load_q(0, s));
-        } else {
-#pragma unroll
-            for (int rt = 0; rt < NR; ++rt) sQ[(rt * 4 + wave) * 64 + lane] = load_q(rt, wave);
-        }
-        int limit[NR];                // row sees key positions t < limit
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            const int r = rt * 16 + l16;
-            limit[rt] = r < R ? min(c + (first_row + r) / G + 1, kend) : 0;
-        }
+            for (int k = 0; k < kQ; ++k) {
+                const int row = grp * kQuantTiles * 16 + (NR == 1 ? 0 : k) * 16 + l16, s = NR == 1 ? k : wave, j = (int)((uint32_t)row * p.g_magic >> 16);
+                r.x[k] = u32x4{0, 0, 0, 0};
+                if (row < p.G * x.n) r.x[k] = *reinterpret_cast<const u32x4*>(p.q + ((size_t)(x.r0 + j) * p.Hq + kvh * p.G + row - j * p.G) * kD + g * 32 + s * 8);
+                r.x[k] ^= p.q_sign;
+            }
+            return r;
+        };
 
         // ---- a step's two pages, HBM -> LDS: 2 direct loads of 1 KB per page.  16-byte chunk ch of K's row (key) r is stored at position ch ^ (r & 7), so that
         // 8 lanes that read the same chunk of 8 rows meet no bank twice; V stays as it is ----
-        unsigned char* ring = smem + wave * kQuantWaveBytes;
         const uint32_t koff = (uint32_t)((lane >> 3) * kD + (((lane & 7) ^ (lane >> 3)) << 4)), voff = (uint32_t)lane * 16;
-        auto issue = [&](int step) {
+        auto issue_as = [&](auto nontemporal, int ids, int step) {
+            constexpr bool STREAM = decltype(nontemporal)::value;
             const int a = __builtin_amdgcn_readlane(ids, 2 * (step & 31)), b = __builtin_amdgcn_readlane(ids, 2 * (step & 31) + 1);
             unsigned char* to = ring + (step & 1) * kQuantStageBytes;
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg) {
                 const size_t at = ((size_t)(pg ? b : a) * p.Hkv + kvh) * kQuantPageBytes;
+                const uint8_t *from_k = scalar_address(p.k + at), *from_v = scalar_address(p.v + at);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    lds_dma16_off(koff, p.k + at + h * 1024, to + pg * kQuantPageBytes + h * 1024);
-                    lds_dma16_off(voff, p.v + at + h * 1024, to + (2 + pg) * kQuantPageBytes + h * 1024);
+                    lds_dma16_off<STREAM>(koff, from_k + h * 1024, to + pg * kQuantPageBytes + h * 1024);
+                    lds_dma16_off<STREAM>(voff, from_v + h * 1024, to + (2 + pg) * kQuantPageBytes + h * 1024);
                 }
             }
+        };
+        auto issue = [&](bool stream, int ids, int step) {
+            if (stream) issue_as(std::true_type{}, ids, step);
+            else issue_as(std::false_type{}, ids, step);
         };
         constexpr int kLoads = 8;                         // of a step
-        const int wkeys = kend - u.kbeg - wave * 32, steps = wkeys <= 0 ? 0 : (wkeys + kQuantStep - 1) / kQuantStep;
-        if (steps > 0) issue(0);
-        if (steps > 1) issue(1);
-        load_scales(0);                                   // (a second round trip that flies with the first pages)
-        if constexpr (NR > 1) __syncthreads();
-        // scales of the two steps in flight: K's of both pages, V's of both pages
-        struct Scales { float k[2], v[2]; };
-        auto scales_of = [&](int step) {
-            Scales x;
+        auto steps_of = [&](const QuantPiece& x) {
+            const int keys = x.kend - x.kbeg - wave * 32;
+            return keys <= 0 ? 0 : (keys + kQuantStep - 1) / kQuantStep;
+        };
+        // scales of one step: of both its pages
+        struct Scales { float ks[2], vm[2], ve[2]; };
+        auto scales_of = [&](const Pages& x, int step) {
+            Scales r;
 #pragma unroll
             for (int pg = 0; pg < 2; ++pg) {
-                x.k[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ksc), 2 * (step & 31) + pg));
-                x.v[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vsc), 2 * (step & 31) + pg));
+                const int l = 2 * (step & 31) + pg;
+                r.ks[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x.ks), l));
+                r.vm[pg] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x.vm), l));
+                r.ve[pg] = TYPE == SPEC_KV_E4M3 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane((int)x.ve, l)) : 1.0f;
             }
-            return x;
+            return r;
         };
-        Scales now = scales_of(0), next = scales_of(1);
 
-        f32x4 o[NR][8];
-        float m_run[NR], l_run[NR];
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            m_run[rt] = kNegBig;
-            l_run[rt] = 0.0f;
-#pragma unroll
-            for (int t = 0; t < 8; ++t) o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
+        Pages pages;
+        pages.id = load_ids(u, 0);
+        bool stream = streams(u, group, look(u));
+        if (steps_of(u) > 0) issue(stream, pages.id, 0);
+        pages = load_scales(u, 0, pages.id);
+        Query query = load_q(u, group);
 
-        auto run = [&](auto active) {
-            constexpr int A = decltype(active)::value;
-            for (int step = 0; step < steps; ++step) {
-                const int wbase = u.kbeg + step * kQuantStep + wave * 32;
-                // this step's pages have landed, the next one's may fly on; once they are in registers, their place is for the step behind that
-                if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
-                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                u32x4 kraw[2][2];
-                u32x2 vraw[2][4];
-                const unsigned char* sK = ring + (step & 1) * kQuantStageBytes;
+        while (true) {
+            const int first_row = group * kQuantTiles * 16, R = min(p.G * u.n - first_row, NR * 16), c = u.c, kend = u.kend, steps = steps_of(u);
+            if constexpr (NR > 1) {
 #pragma unroll
-                for (int pg = 0; pg < 2; ++pg) {
+                for (int rt = 0; rt < NR; ++rt) sQ[(rt * 4 + wave) * 64 + lane] = query.x[rt];
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the first step's pages, with the scales and queries that were requested beside them
+            Scales now = scales_of(pages, 0), nxt = scales_of(pages, 1);
+            if (steps > 1) issue(stream, pages.id, 1);
+            if constexpr (NR > 1) __syncthreads();
+            // what comes next, and its page ids
+            QuantPiece v = u;
+            int v_group = group;
+            const bool more = next(v, v_group);
+            int v_ids = 0;
+            Look v_look{0.0f, false};
+            if (more) {
+                v_ids = load_ids(v, 0);
+                v_look = look(v);
+            }
+
+            int limit[NR];                // row sees key positions t < limit
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) kraw[pg][h] = *reinterpret_cast<const u32x4*>(sK + pg * kQuantPageBytes + l16 * kD + (((2 * g + h) ^ (l16 & 7)) << 4));
+            for (int rt = 0; rt < NR; ++rt) {
+                const int r = rt * 16 + l16;
+                limit[rt] = r < R ? min(c + (int)((uint32_t)(first_row + r) * p.g_magic >> 16) + 1, kend) : 0;
+            }
+            f32x4 o[NR][8];
+            float m_run[NR], l_run[NR];
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) vraw[pg][r] = *reinterpret_cast<const u32x2*>(sK + (2 + pg) * kQuantPageBytes + (4 * g + r) * kD + l16 * 8);
-                }
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                float ks[2] = {now.k[0] * p.scale_log2e, now.k[1] * p.scale_log2e};
-                const float vs[2] = {now.v[0], now.v[1]};
-                now = next;
-                if (step + 2 < steps) {
-                    if (((step + 2) & 31) == 0) {         // the next 32 steps
-                        load_ids(step + 2);
-                        load_scales(step + 2);
+            for (int rt = 0; rt < NR; ++rt) {
+                m_run[rt] = kNegBig;
+                l_run[rt] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < 8; ++t) o[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+
+            auto keys = [&](auto active) {
+                constexpr int A = decltype(active)::value;
+                for (int step = 0; step < steps; ++step) {
+                    const int wbase = u.kbeg + step * kQuantStep + wave * 32;
+                    // this step's pages have landed (the first one's before the loop), the next one's may fly on; once they are in registers, their place is for the
+                    // step behind that
+                    if (step == 0) asm volatile("" ::: "memory");
+                    else if (step + 1 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+                    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    u32x4 kraw[2][2];
+                    u32x2 vraw[2][4];
+                    const unsigned char* sK = ring + (step & 1) * kQuantStageBytes;
+#pragma unroll
+                    for (int pg = 0; pg < 2; ++pg) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) kraw[pg][h] = *reinterpret_cast<const u32x4*>(sK + pg * kQuantPageBytes + l16 * kD + (((2 * g + h) ^ (l16 & 7)) << 4));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) vraw[pg][r] = *reinterpret_cast<const u32x2*>(sK + (2 + pg) * kQuantPageBytes + (4 * g + r) * kD + l16 * 8);
                     }
-                    issue(step + 2);
-                    next = scales_of(step + 2);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                // (two row tiles and more: Q is read again in every step; the compiler would rather keep all of it in registers)
-                int q_lane = lane;
-                if constexpr (NR > 1) asm volatile("" : "+v"(q_lane));
-                // ---- S^T = K Q^T; sc * ks is a score in the log2 domain ----
-                float sc[A][8];
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    float ks[2] = {now.ks[0], now.ks[1]};
+                    const float vm[2] = {now.vm[0], now.vm[1]}, ve[2] = {now.ve[0], now.ve[1]};
+                    now = nxt;
+                    if (step + 2 < steps) {
+                        if (((step + 2) & 31) == 0) pages = load_scales(u, step + 2, load_ids(u, step + 2));     // the next 32 steps
+                        issue(stream, pages.id, step + 2);
+                        nxt = scales_of(pages, step + 2);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    // (two row tiles and more: Q is read again in every step; the compiler would rather keep all of it in registers)
+                    int q_lane = lane;
+                    if constexpr (NR > 1) asm volatile("" : "+v"(q_lane));
+                    // ---- S^T = K Q^T; sc * ks is a score in the log2 domain ----
+                    float sc[A][8];
 #pragma unroll
-                for (int pg = 0; pg < 2; ++pg) {
-                    f32x4 acc[A];
+                    for (int pg = 0; pg < 2; ++pg) {
+                        f32x4 acc[A];
 #pragma unroll
-                    for (int rt = 0; rt < A; ++rt) acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int rt = 0; rt < A; ++rt) acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        const u32x4 raw = kraw[pg][s >> 1];
-                        const bf16x8 kf = (s & 1) ? bf16_oct<TYPE>(raw.z, raw.w) : bf16_oct<TYPE>(raw.x, raw.y);
+                        for (int s = 0; s < 4; ++s) {
+                            const u32x4 raw = kraw[pg][s >> 1];
+                            const bf16x8 kf = (s & 1) ? bf16_oct<TYPE>(raw.z, raw.w) : bf16_oct<TYPE>(raw.x, raw.y);
 #pragma unroll
-                        for (int rt = 0; rt < A; ++rt) {
-                            const bf16x8 qx = NR == 1 ? qf[s] : __builtin_bit_cast(bf16x8, sQ[(rt * 4 + s) * 64 + q_lane]);
-                            acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qx, acc[rt], 0, 0, 0);
+                            for (int rt = 0; rt < A; ++rt) {
+                                const bf16x8 qx = __builtin_bit_cast(bf16x8, NR == 1 ? query.x[NR == 1 ? s : 0] : sQ[(rt * 4 + s) * 64 + q_lane]);
+                                acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qx, acc[rt], 0, 0, 0);
+                            }
+                            __builtin_amdgcn_sched_barrier(0);
                         }
-                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int rt = 0; rt < A; ++rt)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) sc[rt][pg * 4 + e] = acc[rt][e];
                     }
+                    if (wbase + 32 > min(c + 1, kend)) {  // (a scale may be 0: masked scores are scaled ones)
 #pragma unroll
-                    for (int rt = 0; rt < A; ++rt)
+                        for (int rt = 0; rt < A; ++rt)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) sc[rt][pg * 4 + e] = acc[rt][e];
-                }
-                const bool need_mask = wbase + 32 > min(c + 1, kend);
-                if (need_mask) {                          // (a scale may be 0: masked scores are scaled ones)
+                            for (int e = 0; e < 8; ++e)
+                                sc[rt][e] = wbase + (e >> 2) * 16 + g * 4 + (e & 3) < limit[rt] ? sc[rt][e] * ks[e >> 2] : kMasked;
+                        ks[0] = ks[1] = 1.0f;
+                    }
+                    // The reference maximum moves only when a score exceeds it by more than kMaxSlack, so exp2(s - m_run) <= 2^kMaxSlack stays well inside fp32 and bf16 and O
+                    // is rescaled a handful of times (the result is the same softmax: O and l carry the same factor).  A lane looks at its own 8 scores, and the four
+                    // lanes of a query row agree on a new maximum where one of them asks for it.
+                    float tmax[A];
+                    bool grow = false;
 #pragma unroll
-                    for (int rt = 0; rt < A; ++rt)
+                    for (int rt = 0; rt < A; ++rt) {
+                        const float a = fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])), b = fmaxf(fmaxf(sc[rt][4], sc[rt][5]), fmaxf(sc[rt][6], sc[rt][7]));
+                        tmax[rt] = fmaxf(a * ks[0], b * ks[1]);
+                        grow |= tmax[rt] > m_run[rt] + kMaxSlack;
+                    }
+                    if (__any(grow)) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            sc[rt][e] = wbase + (e >> 2) * 16 + g * 4 + (e & 3) < limit[rt] ? sc[rt][e] * ks[e >> 2] : kNegBig;
-                    ks[0] = ks[1] = 1.0f;
-                }
-                // The reference maximum moves only when a score exceeds it by more than kMaxSlack, so exp2(s - m_run) <= 2^kMaxSlack stays well inside fp32 and bf16 and O
-                // is rescaled a handful of times (the result is the same softmax: O and l carry the same factor).  A lane looks at its own 8 scores, and the four lanes
-                // of a query row agree on a new maximum where one of them asks for it.
-                float tmax[A];
-                bool grow = false;
+                        for (int rt = 0; rt < A; ++rt)
+                            if (__any(tmax[rt] > m_run[rt] + kMaxSlack)) {
+                                const float m_new = fmaxf(m_run[rt], four_rows_max(tmax[rt]));
+                                const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+                                m_run[rt] = m_new;
+                                l_run[rt] *= alpha;
 #pragma unroll
-                for (int rt = 0; rt < A; ++rt) {
-                    const float a = fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])), b = fmaxf(fmaxf(sc[rt][4], sc[rt][5]), fmaxf(sc[rt][6], sc[rt][7]));
-                    tmax[rt] = fmaxf(a * ks[0], b * ks[1]);
-                    grow |= tmax[rt] > m_run[rt] + kMaxSlack;
-                }
-                if (__any(grow)) {
+                                for (int t = 0; t < 8; ++t) o[rt][t] *= alpha;
+                            }
+                    }
+                    float pr[A][8];
 #pragma unroll
-                    for (int rt = 0; rt < A; ++rt)
-                        if (__any(tmax[rt] > m_run[rt] + kMaxSlack)) {
-                            const float m_new = fmaxf(m_run[rt], four_rows_max(tmax[rt]));
-                            const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
-                            m_run[rt] = m_new;
-                            l_run[rt] *= alpha;
+                    for (int rt = 0; rt < A; ++rt) {
+                        float psum = 0.0f;
 #pragma unroll
-                            for (int t = 0; t < 8; ++t) o[rt][t] *= alpha;
+                        for (int e = 0; e < 8; ++e) {
+                            // (masked: 0, also in a row that has seen nothing, whose m_run is kNegBig)
+                            pr[rt][e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
+                            psum += pr[rt][e];
                         }
-                }
-                bf16x8 pf[A];
-#pragma unroll
-                for (int rt = 0; rt < A; ++rt) {
-                    float pr[8], psum = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        pr[e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
-                        // (a row that has seen nothing at all has m_run == kNegBig)
-                        if (need_mask) pr[e] = sc[rt][e] > 0.5f * kNegBig ? pr[e] : 0.0f;
-                        psum += pr[e];
+                        l_run[rt] += psum;
                     }
-                    l_run[rt] += psum;
-                    const u32x4 pw = {pack_bf16x2(pr[0] * vs[0], pr[1] * vs[0]), pack_bf16x2(pr[2] * vs[0], pr[3] * vs[0]),
-                                      pack_bf16x2(pr[4] * vs[1], pr[5] * vs[1]), pack_bf16x2(pr[6] * vs[1], pr[7] * vs[1])};
-                    pf[rt] = __builtin_bit_cast(bf16x8, pw);
-                }
-                // ---- O^T += V^T P^T ----
-                if (wbase + 32 > kend) {
-                    // slots past the range may hold anything (even NaN patterns): P is 0 there, so V must be too
+                    if (vm[0] != 1.0f || vm[1] != 1.0f) {
+#pragma unroll
+                        for (int rt = 0; rt < A; ++rt)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) pr[rt][e] *= vm[e >> 2];
+                    }
+                    bf16x8 pf[A];
+#pragma unroll
+                    for (int rt = 0; rt < A; ++rt) {
+                        const u32x4 pw = {pack_bf16x2(pr[rt][0], pr[rt][1]), pack_bf16x2(pr[rt][2], pr[rt][3]), pack_bf16x2(pr[rt][4], pr[rt][5]), pack_bf16x2(pr[rt][6], pr[rt][7])};
+                        pf[rt] = __builtin_bit_cast(bf16x8, pw);
+                    }
+                    // ---- O^T += V^T P^T ----
+                    if (wbase + 32 > kend) {
+                        // slots past the range may hold anything (even NaN patterns): P is 0 there, so V must be too
+#pragma unroll
+                        for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (wbase + pg * 16 + g * 4 + r >= kend) vraw[pg][r] = u32x2{0, 0};
+                    }
+                    uint32_t pair[2][2][4];               // [page][keys 4g, 4g+1 | 4g+2, 4g+3][t / 2]: bytes {key a, key b} of t, then of t + 1
 #pragma unroll
                     for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (wbase + pg * 16 + g * 4 + r >= kend) vraw[pg][r] = u32x2{0, 0};
-                }
-                uint32_t pair[2][2][4];                   // [page][keys 4g, 4g+1 | 4g+2, 4g+3][t / 2]: bytes {key a, key b} of t, then of t + 1
+                        for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
-                for (int pg = 0; pg < 2; ++pg)
-#pragma unroll
-                    for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            uint32_t a = w ? vraw[pg][2 * k2].y : vraw[pg][2 * k2].x, b = w ? vraw[pg][2 * k2 + 1].y : vraw[pg][2 * k2 + 1].x;
-                            asm("" : "+v"(a), "+v"(b));
-                            pair[pg][k2][2 * w] = __builtin_amdgcn_perm(b, a, 0x05010400u);
-                            pair[pg][k2][2 * w + 1] = __builtin_amdgcn_perm(b, a, 0x07030602u);
-                        }
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    u32x4 w;
-                    if (t & 1) w = u32x4{bf16_pair<TYPE, true>(pair[0][0][t >> 1]), bf16_pair<TYPE, true>(pair[0][1][t >> 1]),
-                                         bf16_pair<TYPE, true>(pair[1][0][t >> 1]), bf16_pair<TYPE, true>(pair[1][1][t >> 1])};
-                    else w = u32x4{bf16_pair<TYPE, false>(pair[0][0][t >> 1]), bf16_pair<TYPE, false>(pair[0][1][t >> 1]),
-                                   bf16_pair<TYPE, false>(pair[1][0][t >> 1]), bf16_pair<TYPE, false>(pair[1][1][t >> 1])};
-                    const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-                    for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o[rt][t], 0, 0, 0);
+                            for (int w = 0; w < 2; ++w) {
+                                uint32_t a = w ? vraw[pg][2 * k2].y : vraw[pg][2 * k2].x, b = w ? vraw[pg][2 * k2 + 1].y : vraw[pg][2 * k2 + 1].x;
+                                asm("" : "+v"(a), "+v"(b));
+                                pair[pg][k2][2 * w] = __builtin_amdgcn_perm(b, a, 0x05010400u);
+                                pair[pg][k2][2 * w + 1] = __builtin_amdgcn_perm(b, a, 0x07030602u);
+                            }
                     __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {
+                        u32x4 w;
+                        if (t & 1) w = u32x4{bf16_pair<TYPE, true>(pair[0][0][t >> 1], ve[0]), bf16_pair<TYPE, true>(pair[0][1][t >> 1], ve[0]),
+                                             bf16_pair<TYPE, true>(pair[1][0][t >> 1], ve[1]), bf16_pair<TYPE, true>(pair[1][1][t >> 1], ve[1])};
+                        else w = u32x4{bf16_pair<TYPE, false>(pair[0][0][t >> 1], ve[0]), bf16_pair<TYPE, false>(pair[0][1][t >> 1], ve[0]),
+                                       bf16_pair<TYPE, false>(pair[1][0][t >> 1], ve[1]), bf16_pair<TYPE, false>(pair[1][1][t >> 1], ve[1])};
+                        const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
+#pragma unroll
+                        for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o[rt][t], 0, 0, 0);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-            }
-        };
-        if (NR >= 3 && R > 32) run(std::integral_constant<int, NR >= 3 ? 3 : 1>{});
-        else if (NR >= 2 && R > 16) run(std::integral_constant<int, NR >= 2 ? 2 : 1>{});
-        else run(std::integral_constant<int, 1>{});
-        if (bad_page && p.status_flags) atomicOr(p.status_flags, SPEC_FLAG_BAD_PAGE);
+            };
+            if (NR >= 3 && R > 32) keys(std::integral_constant<int, NR >= 3 ? 3 : 1>{});
+            else if (NR >= 2 && R > 16) keys(std::integral_constant<int, NR >= 2 ? 2 : 1>{});
+            else keys(std::integral_constant<int, 1>{});
 
-        // ---- merge the waves, in slices of d: each leaves its O where its pages were (16-byte chunk c of a row at position c ^ (row & 7)), maxima and sums beside; a thread then
-        // takes 4 consecutive d of a row from all waves ----
-        float* own = reinterpret_cast<float*>(ring);
-#pragma unroll
-        for (int rt = 0; rt < NR; ++rt) {
-            const float l = four_rows_sum(l_run[rt]);
-            if (g == 0) {
-                s_m[wave * NR * 16 + rt * 16 + l16] = m_run[rt];
-                s_l[wave * NR * 16 + rt * 16 + l16] = l;
+            // ---- the next piece's scales, queries and first step ----
+            if (more) {
+                pages = load_scales(v, 0, v_ids);
+                query = load_q(v, v_group);
+                stream = streams(v, v_group, v_look);
+                if (steps_of(v) > 0) issue(stream, v_ids, 0);
             }
-        }
+            // ---- merge the waves, a row tile at a time: each leaves its O where the pages of its second step were (16-byte chunk c of a row at position
+            // c ^ (row & 7)), maxima and sums beside; a thread then takes 4 consecutive d of a row from all waves ----
+            float* own = reinterpret_cast<float*>(ring + kQuantStageBytes);
 #pragma unroll
-        for (int sl = 0; sl < kSlices; ++sl) {
-            if (sl > 0) __syncthreads();                  // everybody has read the previous slice
-            if (32 * g / kSliceD == sl) {
+            for (int rt = 0; rt < NR; ++rt) {
+                const float l = four_rows_sum(l_run[rt]);
+                if (g == 0) {
+                    s_m[wave * NR * 16 + rt * 16 + l16] = m_run[rt];
+                    s_l[wave * NR * 16 + rt * 16 + l16] = l;
+                }
+            }
 #pragma unroll
-                for (int rt = 0; rt < NR; ++rt)
+            for (int rt = 0; rt < NR; ++rt) {
+                if (rt * 16 >= R) break;
+                if (rt > 0) __syncthreads();              // everybody has read the previous tile
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            // d = 32 g + 8 e + 4 w .. + 3
-                            const int ch = (32 * g % kSliceD) / 4 + 2 * e + w;
-                            *reinterpret_cast<f32x4*>(own + (rt * 16 + l16) * kSliceD + ((ch ^ (l16 & 7)) << 2)) =
-                                f32x4{o[rt][4 * w][e], o[rt][4 * w + 1][e], o[rt][4 * w + 2][e], o[rt][4 * w + 3][e]};
+                    for (int w = 0; w < 2; ++w) {
+                        // d = 32 g + 8 e + 4 w .. + 3
+                        const int ch = 8 * g + 2 * e + w;
+                        *reinterpret_cast<f32x4*>(own + l16 * kD + ((ch ^ (l16 & 7)) << 2)) =
+                            f32x4{o[rt][4 * w][e], o[rt][4 * w + 1][e], o[rt][4 * w + 2][e], o[rt][4 * w + 3][e]};
+                    }
+                __syncthreads();
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int at = half * 8 + (tid >> 5), r = rt * 16 + at, ch = tid & 31;
+                    if (r < R) {
+                        float m[NW], mx = kNegBig;
+#pragma unroll
+                        for (int w = 0; w < NW; ++w) {
+                            m[w] = s_m[w * NR * 16 + r];
+                            mx = fmaxf(mx, m[w]);
                         }
-            }
-            __syncthreads();
-            for (int e = tid; e < R * kChunks; e += kQuantThreads) {
-                const int r = e / kChunks, ch = e % kChunks;
-                float m[NW], mx = kNegBig;
+                        f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
+                        float l = 0.0f;
 #pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    m[w] = s_m[w * NR * 16 + r];
-                    mx = fmaxf(mx, m[w]);
-                }
-                f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
-                float l = 0.0f;
-#pragma unroll
-                for (int w = 0; w < NW; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(m[w] - mx);
-                    num += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * kQuantWaveBytes) + r * kSliceD + ((ch ^ (r & 7)) << 2));
-                    l += f * s_l[w * NR * 16 + r];
-                }
-                const int j = (first_row + r) / G, gq = first_row + r - j * G;
-                if (u.whole) {
-                    const size_t rowhead = (size_t)(u.r0 + j) * p.Hq + kvh * G + gq;
-                    u32x2_any packed;
-                    packed.x = pack_bf16x2(num.x / l, num.y / l);
-                    packed.y = pack_bf16x2(num.z / l, num.w / l);
-                    *reinterpret_cast<u32x2_any*>(p.out + rowhead * kD + sl * kSliceD + ch * 4) = packed;
-                    if (p.lse && sl == 0 && ch == 0) p.lse[rowhead] = (mx + log2f(l)) * 0.6931471805599453f;
-                } else {
-                    const size_t at = (u.slot * p.max_q_len + j) * p.Hq + kvh * G + gq;
-                    *reinterpret_cast<f32x4*>(p.part_o + at * kD + sl * kSliceD + ch * 4) = num;
-                    if (sl == 0 && ch == 0) { p.part_m[at] = mx; p.part_l[at] = l; }
+                        for (int w = 0; w < NW; ++w) {
+                            const float f = __builtin_amdgcn_exp2f(m[w] - mx);
+                            num += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(smem + w * kQuantWaveBytes + kQuantStageBytes) + at * kD + ((ch ^ (at & 7)) << 2));
+                            l += f * s_l[w * NR * 16 + r];
+                        }
+                        const int j = (int)((uint32_t)(first_row + r) * p.g_magic >> 16), hq = kvh * p.G + first_row + r - j * p.G;
+                        if (u.whole) {
+                            const size_t rowhead = (size_t)(u.r0 + j) * p.Hq + hq;
+                            const float inv = 1.0f / l;
+                            u32x2_any packed;
+                            packed.x = pack_bf16x2(num.x * inv, num.y * inv);
+                            packed.y = pack_bf16x2(num.z * inv, num.w * inv);
+                            *reinterpret_cast<u32x2_any*>(p.out + rowhead * kD + ch * 4) = packed;
+                            if (p.lse && ch == 0) p.lse[rowhead] = (mx + log2f(l)) * 0.6931471805599453f;
+                        } else {
+                            const size_t slot = (u.slot * p.max_q_len + j) * p.Hq + hq;
+                            *reinterpret_cast<f32x4*>(p.part_o + slot * kD + ch * 4) = num;
+                            if (ch == 0) { p.part_m[slot] = mx; p.part_l[slot] = l; }
+                        }
+                    }
                 }
             }
+            if (!more) break;
+            u = v;
+            group = v_group;
+            pages.id = v_ids;
+            __syncthreads();                              // Q and the place of the second step are free again
         }
+        if (bad_page && p.status_flags) atomicOr(p.status_flags, SPEC_FLAG_BAD_PAGE);
     }
 };
 
@@ -439,23 +535,41 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
     typedef QuantKernel<NR, TYPE> Kernel;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if constexpr (!RANGES) {
-        const int group = blockIdx.x / p.Hkv, kvh = blockIdx.x - group * p.Hkv, i = blockIdx.y;
+        const int group = blockIdx.x / p.Hkv, kvh = blockIdx.x - group * p.Hkv;
+        int i = blockIdx.y;
+        if (p.by_length) {
+            // workgroups start in grid order: the longest requests first (ties: request order), so that short ones fill the end
+            uint32_t* s_key = reinterpret_cast<uint32_t*>(smem);      // [kQuantOrdered], then the request
+            const uint32_t key = tid < p.B ? (uint32_t)min(max(p.seq_lens[tid], 0), (1 << 23) - 1) << 8 | (uint32_t)(kQuantOrdered - 1 - tid) : 0;
+            s_key[tid] = key;
+            __syncthreads();
+            int above = 0;
+#pragma unroll 4
+            for (int k = 0; k < kQuantOrdered; k += 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(s_key + k);
+                above += (x.x > key) + (x.y > key) + (x.z > key) + (x.w > key);
+            }
+            if (tid < p.B && above == i) s_key[kQuantOrdered] = (uint32_t)tid;
+            __syncthreads();
+            i = __builtin_amdgcn_readfirstlane((int)s_key[kQuantOrdered]);
+            __syncthreads();                              // (pages land there next)
+        }
         const auto [r0, n, c] = quant_request(p, i);
         if (!quant_request_ok(r0, n, c, p)) {
             if (blockIdx.x == 0 && tid == 0 && p.status_flags) atomicOr(p.status_flags, SPEC_FLAG_BAD_LENGTH);
             return;
         }
-        const QuantPiece u{i, r0, n, c, 0, c + n, true, 0};
-        for (int at = group; at * kQuantTiles * 16 < p.G * n; at += p.groups) {
-            if (at > group) __syncthreads();              // the buffers are free again
-            Kernel::piece(p, smem, u, kvh, at);
-        }
+        if (group * kQuantTiles * 16 >= p.G * n) return;
+        Kernel::run(p, smem, kvh, QuantPiece{i, r0, n, c, 0, c + n, true, 0}, group, [&](QuantPiece& u, int& at) {
+            at += p.groups;
+            return at * kQuantTiles * 16 < p.G * u.n;
+        });
     } else {
         const int kvh = blockIdx.x, range = blockIdx.y;
         // Every request's work and what comes before it, four requests per thread; the total gives the size of a range, and the request in which this one starts leaves its
         // number and place in LDS.
         constexpr int kPer = kQuantListed / kQuantThreads;
-        int* s_scan = reinterpret_cast<int*>(smem);       // [8], then {request, work before it}
+        int* s_scan = reinterpret_cast<int*>(smem);       // [4], then {request, work before it}
         int work[kPer], mine = 0;
         bool bad = false;
 #pragma unroll
@@ -464,7 +578,7 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
             work[k] = 0;
             if (i < p.B) {
                 const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
-                if (quant_request_ok(r0, n, c, p)) work[k] = (c + n + kQuantStep - 1) / kQuantStep * quant_step_work(p.G * n);
+                if (quant_request_ok(r0, n, c, p)) work[k] = quant_piece_work(p.G * n) + (c + n + kQuantStep - 1) / kQuantStep * quant_step_work(p.G * n);
                 else bad = true;
             }
             mine += work[k];
@@ -486,7 +600,7 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
         }
         total = __builtin_amdgcn_readfirstlane(total);
         const int quantum = max(p.min_work, (total + p.ranges - 1) / p.ranges);
-        const int first = range * quantum, last = min(total, first + quantum);        // (at most total + ranges * min_work: the host sees to 32 bits)
+        const int first = range * quantum, last = min(total, first + quantum);        // (32 bits hold them: see quant_plan)
         if (first >= total) return;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
@@ -494,27 +608,36 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
             before += work[k];
         }
         __syncthreads();
-        int i = __builtin_amdgcn_readfirstlane(s_scan[4]), at = __builtin_amdgcn_readfirstlane(s_scan[5]);      // `at`: the work before request i
-        while (at < last) {
-            __syncthreads();                              // the buffers are free again
-            const auto [r0, n, c] = quant_request(p, i);
-            if (quant_request_ok(r0, n, c, p)) {
-                const int len = c + n, steps = (len + kQuantStep - 1) / kQuantStep, w = quant_step_work(p.G * n);
-                // the steps whose place lies in this range
-                const int from = at >= first ? 0 : (first - at + w - 1) / w, to = min(steps, (first + quantum - at + w - 1) / w);
-                const int head = at / quantum, pieces = (at + (steps - 1) * w) / quantum - head + 1;
-                if (from == 0 && kvh == 0 && tid == 0) p.req[i] = u32x2{(uint32_t)head, (uint32_t)pieces};
-                if (from < to) {
-                    const QuantPiece u{i, r0, n, c, from * kQuantStep, min(len, to * kQuantStep), pieces == 1, 2 * (size_t)range + (from == 0)};
-                    for (int group = 0; group * kQuantTiles * 16 < p.G * n; ++group) {
-                        if (group > 0) __syncthreads();
-                        Kernel::piece(p, smem, u, kvh, group);
+        int i = __builtin_amdgcn_readfirstlane(s_scan[4]), at = __builtin_amdgcn_readfirstlane(s_scan[5]);      // request, and the work before it
+        __syncthreads();                                  // (pages land there next)
+        // the next request with steps in this range, whole or in part
+        auto piece_from = [&](QuantPiece& u) {
+            while (at < last) {
+                const auto [r0, n, c] = quant_request(p, i);
+                if (quant_request_ok(r0, n, c, p)) {
+                    const int len = c + n, steps = (len + kQuantStep - 1) / kQuantStep, w = quant_step_work(p.G * n);
+                    // the steps whose place lies in this range
+                    const int begin = at + quant_piece_work(p.G * n);        // the place of its first step
+                    const int from = begin >= first ? 0 : (first - begin + w - 1) / w, to = min(steps, max(0, first + quantum - begin + w - 1) / w);
+                    const int head = begin / quantum, pieces = (begin + (steps - 1) * w) / quantum - head + 1;
+                    if (from == 0 && kvh == 0 && tid == 0) p.req[i] = u32x2{(uint32_t)head, (uint32_t)pieces};
+                    at = begin + steps * w;
+                    if (from < to) {
+                        u = QuantPiece{i++, r0, n, c, from * kQuantStep, min(len, to * kQuantStep), pieces == 1, 2 * (size_t)range + (from == 0)};
+                        return true;
                     }
                 }
-                at += steps * w;
+                ++i;
             }
-            ++i;
-        }
+            return false;
+        };
+        QuantPiece u;
+        if (!piece_from(u)) return;
+        Kernel::run(p, smem, kvh, u, 0, [&](QuantPiece& v, int& group) {
+            if (++group * kQuantTiles * 16 < p.G * v.n) return true;
+            group = 0;
+            return piece_from(v);
+        });
     }
 }
 
@@ -593,6 +716,7 @@ __global__ __launch_bounds__(256) void verify_attn_quant_merge_kernel(QuantAttnP
 struct QuantPlan {
     int tiles, groups;                       // row tiles at once, workgroups per request and kv head (whole requests)
     int ranges, min_work;                    // 0 ranges: whole requests
+    bool by_length;                          // whole requests: the longest first
     bool many;                               // pieces per request: a workgroup per head merges them
     size_t slots, req_bytes;
 };
@@ -607,10 +731,20 @@ static QuantPlan quant_plan(int B, int Hq, int Hkv, int max_kv_len, int max_q_le
     const int row_groups = (NR + kQuantTiles - 1) / kQuantTiles;
     const long cus = device_cu_count(), units = (long)B * Hkv;
     c.groups = units >= cus ? 1 : row_groups;
+    c.by_length = B > 1 && B <= kQuantOrdered && units > cus;
     const int mode = g_attn_plan, chunk = g_attn_chunk_override, waves = g_attn_plan_waves;
     const long steps = ((long)max_kv_len + kQuantStep - 1) / kQuantStep, work = quant_step_work(G * max_q_len);
-    const long most = B * steps * work;      // work of the batch at its bounds
-    if (mode == 2 || B > kQuantListed || steps < 2 * kQuantMinSteps || most > (1L << 30)) return c;
+    const long most = B * (steps * work + quant_piece_work(G * max_q_len));            // work of the batch at its bounds
+    if (mode == 2 || B > kQuantListed || most > (1L << 30)) return c;
+    // Whole requests need no merge and leave no bubbles between pieces, but the longest one is as long as the call.  In us: what it takes (0.8, 1.3, 1.6 a step with 1, 2, 3 row
+    // tiles) against what the ranges' second launch and partials cost (8, with more than one row tile 18 once the chip is busy) and half of what the batch takes at its bounds and
+    // 6.5 TB/s (lengths are usually below them).  Ranges / whole, us, all requests at the bound | lengths from an eighth of it on, 1 row tile: 1 x 1024 keys 13.1 / 12.0, 2048 14.0 / 18.4;
+    // 128 requests x heads of 2048 24.4 / 20.6 | 20.0 / 19.5, 4096 34.9 / 34.7 | 25.7 / 32.6; 256 of 4096 57.5 / 48.1 | 38.3 / 35.2, 8192 101 / 90 | 63 / 66; 3 row tiles: 1 x 512
+    // 17.3 / 15.0, 1024 17.5 / 21.4; 128 of 2048 37.1 / 37.0 | 30.4 / 35.1; 256 of 2048 51.6 / 40.6 | 40.5 / 38.0, 4096 78 / 67 | 56 / 63.
+    const double all_us = (double)units * max_kv_len * (2 * kD) / 6.5e6;
+    const double one_us = steps * (NR == 1 ? 0.8 : NR == 2 ? 1.3 : 1.6 * row_groups);
+    const double saved_us = 8.0 + (NR == 1 ? 0.0 : 10.0 * std::min(1.0, all_us / 15.0));
+    if (mode != 1 && chunk <= 0 && one_us <= saved_us + 0.5 * all_us) return c;
     c.min_work = (int)(kQuantMinSteps * work);
     long ranges = std::max<long>(1, cus * (waves > 0 ? waves : kQuantWgsPerCu) / Hkv);
     if (chunk > 0) { ranges = (long)B * max_kv_len / chunk + 1; c.min_work = (int)work; }
@@ -697,7 +831,11 @@ extern "C" int spec_verify_attn_quantized(const void* q, const void* k_cache, co
     p.out = (uint16_t*)out; p.lse = lse; p.status_flags = status_flags;
     p.max_pages = max_pages_per_seq; p.num_pages = num_pages; p.Hq = Hq; p.Hkv = Hkv; p.G = G;
     p.M = M; p.B = B; p.max_kv_len = max_kv_len; p.max_q_len = max_q_len;
-    p.ranges = c.ranges; p.min_work = c.min_work; p.groups = c.groups;
+    p.ranges = c.ranges; p.min_work = c.min_work; p.groups = c.groups; p.by_length = c.by_length;
+    // 3/8 of the cache.  Calls on three batches in turn, ordinary -> nontemporal: 21 MB 43.7 -> 47 us, 101 MB 50 -> 47, 134 MB 34 -> 30, 680 MB 143 -> 128
+    const int near = std::min(B, kKvScanRequests);
+    p.stream_keys = (float)(kMemorySideCache / (2 * kD) * 3 / 8) / (float)Hkv * (float)((near + 3) / 4) / (float)near;       // (what the looked-at quarter adds up to)
+    p.g_magic = 65536u / (uint32_t)G + 1;
     p.scale_log2e = fabsf(scale) * 1.4426950408889634f;
     p.q_sign = scale < 0.0f ? 0x80008000u : 0u;
     hipStream_t s = (hipStream_t)stream;
