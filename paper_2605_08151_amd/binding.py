@@ -413,25 +413,7 @@ def spec_kv_commit_tree(k_cache, v_cache, page_table, seq_lens, qo_indptr, accep
 
 # element types of a cache in 8 bits
 KV_TYPES = {torch.float8_e4m3fn: 0, torch.int8: 1}
-
-
-def _cache_pair(k_cache, v_cache, k_scale, v_scale):
-    """(num_pages, Hkv, page size, D, type) of an 8-bit cache."""
-    num_pages, Hkv, P, D = k_cache.shape
-    assert k_cache.dtype in KV_TYPES and v_cache.shape == k_cache.shape, (k_cache.dtype, k_cache.shape, v_cache.shape)
-    assert tuple(k_scale.shape) == (num_pages, Hkv) and tuple(v_scale.shape) == (num_pages, Hkv), (k_scale.shape, v_scale.shape)
-    return num_pages, Hkv, P, D, KV_TYPES[k_cache.dtype]
-
-
-def _row_pair(k, v, Hkv, D):
-    """(rows, stride between rows) of K/V rows [M, Hkv, D] bf16 that are contiguous inside a row and lie equally far apart."""
-    M = k.shape[0]
-    assert tuple(k.shape) == (M, Hkv, D) and v.shape == k.shape, (k.shape, v.shape)
-    assert k.is_cuda and v.is_cuda and k.dtype == v.dtype == torch.bfloat16, (k.dtype, v.dtype)
-    stride = k.stride(0) if M > 1 else Hkv * D
-    for t in (k, v):
-        assert t.stride(2) == 1 and (Hkv == 1 or t.stride(1) == D) and (M <= 1 or t.stride(0) == stride), (k.stride(), v.stride())
-    return M, stride
+_quantized_cache, _kv_rows = _marshal.quantized_cache, _marshal.kv_rows
 
 
 def spec_kv_reserve_workspace_bytes(B):
@@ -450,22 +432,20 @@ def spec_kv_reserve(page_table, num_pages, seq_lens, qo_indptr, free_list, free_
 
 def spec_kv_quantize(k, v, slot_map, k_cache, v_cache, k_scale, v_scale, status_flags):
     """k, v [M, Hkv, D] bf16, rows possibly strided (slices of a projection's output); k_cache, v_cache float8_e4m3fn or int8."""
-    num_pages, Hkv, P, D, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
-    M, stride = _row_pair(k, v, Hkv, D)
+    num_pages, Hkv, P, D, kv_type, kc, vc, ks, vs = _quantized_cache(k_cache, v_cache, k_scale, v_scale)
+    M, stride, k_rows, v_rows = _kv_rows(k, v, Hkv, D)
     assert slot_map.shape[0] == M
-    _check(_lib.spec_kv_quantize(
-        k.data_ptr(), v.data_ptr(), stride, _ptr(slot_map, torch.int32), _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32),
-        _ptr(v_scale, torch.float32), num_pages, M, Hkv, D, P, kv_type, _ptr(status_flags, torch.int32), _stream()))
+    _check(_lib.spec_kv_quantize(k_rows, v_rows, stride, _ptr(slot_map, torch.int32), kc, vc, ks, vs, num_pages, M, Hkv, D, P, kv_type,
+                                 _ptr(status_flags, torch.int32), _stream()))
 
 
 def spec_kv_dequantize(k_cache, v_cache, k_scale, v_scale, slot_map, k, v, status_flags):
     """k, v [M, Hkv, D] bf16 as for spec_kv_quantize."""
-    num_pages, Hkv, P, D, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
-    M, stride = _row_pair(k, v, Hkv, D)
+    num_pages, Hkv, P, D, kv_type, kc, vc, ks, vs = _quantized_cache(k_cache, v_cache, k_scale, v_scale)
+    M, stride, k_rows, v_rows = _kv_rows(k, v, Hkv, D)
     assert slot_map.shape[0] == M
-    _check(_lib.spec_kv_dequantize(
-        _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), num_pages, _ptr(slot_map, torch.int32),
-        k.data_ptr(), v.data_ptr(), stride, M, Hkv, D, P, kv_type, _ptr(status_flags, torch.int32), _stream()))
+    _check(_lib.spec_kv_dequantize(kc, vc, ks, vs, num_pages, _ptr(slot_map, torch.int32), k_rows, v_rows, stride, M, Hkv, D, P, kv_type,
+                                   _ptr(status_flags, torch.int32), _stream()))
 
 
 def spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, max_q_len):
@@ -475,12 +455,11 @@ def spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, max
 def spec_verify_attn_quantized(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, out, lse, max_kv_len, max_q_len, scale,
                                status_flags, workspace):
     M, Hq, D = q.shape
-    num_pages, Hkv, P, Dk, kv_type = _cache_pair(k_cache, v_cache, k_scale, v_scale)
-    B = seq_lens.shape[0]
-    assert Dk == D and page_table.shape[0] == B and qo_indptr.shape[0] == B + 1 and out.shape == q.shape and (lse is None or tuple(lse.shape) == (M, Hq))
+    num_pages, Hkv, P, Dk, kv_type, kc, vc, ks, vs = _quantized_cache(k_cache, v_cache, k_scale, v_scale)
+    B, max_pages = page_table.shape
+    assert Dk == D and seq_lens.shape[0] == B and qo_indptr.shape[0] == B + 1 and out.shape == q.shape and (lse is None or lse.shape == (M, Hq))
     _check(_lib.spec_verify_attn_quantized(
-        _ptr(q, torch.bfloat16), _ptr(k_cache), _ptr(v_cache, k_cache.dtype), _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32),
-        _ptr(page_table, torch.int32), page_table.shape[1], num_pages, _ptr(seq_lens, torch.int32),
+        _ptr(q, torch.bfloat16), kc, vc, ks, vs, _ptr(page_table, torch.int32), max_pages, num_pages, _ptr(seq_lens, torch.int32),
         _ptr(qo_indptr, torch.int32), _ptr(out, torch.bfloat16), _ptr(lse, torch.float32),
         B, M, Hq, Hkv, D, P, kv_type, int(max_kv_len), int(max_q_len), float(scale), _ptr(status_flags, torch.int32),
         _ptr(workspace), workspace.numel() * workspace.element_size() if workspace is not None else 0, _stream()))

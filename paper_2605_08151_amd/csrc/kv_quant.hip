@@ -68,6 +68,21 @@ __device__ inline float power_scale(float amax)
     return bits == 0 ? 0.0f : __builtin_bit_cast(float, (uint32_t)e << 23);
 }
 
+// Loads and stores of operands that are touched once, nontemporal where a call is too large for the memory-side cache.
+template <bool STREAM, typename T>
+__device__ inline T load_once(const void* at)
+{
+    if constexpr (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
+    else return *reinterpret_cast<const T*>(at);
+}
+
+template <bool STREAM, typename T>
+__device__ inline void store_once(void* at, T x)
+{
+    if constexpr (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<T*>(at));
+    else *reinterpret_cast<T*>(at) = x;
+}
+
 struct QuantParams {
     const uint16_t* x[2];    // K, V rows
     uint8_t* cache[2];
@@ -79,7 +94,7 @@ struct QuantParams {
 };
 
 // WINDOW: rows whose runs a wave looks for.
-template <int TYPE, int WINDOW>
+template <int TYPE, int WINDOW, bool STREAM>
 __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantParams p)
 {
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
@@ -118,7 +133,7 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantParams p)
         for (int q = 0; q < 4; ++q) {
             v[q] = u32x4{0, 0, 0, 0};
             held[q] = u32x2{0, 0};
-            if (q * 4 + g < len) v[q] = *reinterpret_cast<const u32x4*>(x + (r0 + q * 4 + g) * p.row_stride + (long)h * kQD + l16 * 8);
+            if (q * 4 + g < len) v[q] = load_once<STREAM, u32x4>(x + (r0 + q * 4 + g) * p.row_stride + (long)h * kQD + l16 * 8);
             if (q * 4 + g < o) held[q] = *reinterpret_cast<const u32x2*>(to + (q * 4 + g) * kQD);
         }
         uint32_t top = 0;
@@ -156,7 +171,7 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantParams p)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] /= now;
                 }
-                *reinterpret_cast<u32x2*>(to + (o + q * 4 + g) * kQD) = pack8<TYPE>(f);
+                store_once<STREAM>(to + (o + q * 4 + g) * kQD, pack8<TYPE>(f));
             }
         if (now > old) {
             const float ratio = old * inverse;            // now is a power of two here
@@ -185,7 +200,7 @@ struct DequantParams {
     int M, Hkv, slots;
 };
 
-template <int TYPE>
+template <int TYPE, bool STREAM>
 __global__ __launch_bounds__(256) void kv_dequantize_kernel(DequantParams p)
 {
     const int l16 = threadIdx.x & 15, which = blockIdx.y;
@@ -199,13 +214,13 @@ __global__ __launch_bounds__(256) void kv_dequantize_kernel(DequantParams p)
         return;
     }
     const size_t unit = (size_t)(slot / kQP) * p.Hkv + h;
-    const u32x2 raw = *reinterpret_cast<const u32x2*>(p.cache[which] + (unit * kQP + slot % kQP) * kQD + l16 * 8);
+    const u32x2 raw = load_once<STREAM, u32x2>(p.cache[which] + (unit * kQP + slot % kQP) * kQD + l16 * 8);
     const float scale = p.scale[which][unit];
     float f[8];
     unpack8<TYPE>(raw, f);
     const u32x4 out = {pack_bf16x2(f[0] * scale, f[1] * scale), pack_bf16x2(f[2] * scale, f[3] * scale),
                        pack_bf16x2(f[4] * scale, f[5] * scale), pack_bf16x2(f[6] * scale, f[7] * scale)};
-    *reinterpret_cast<u32x4*>(p.out[which] + (long)row * p.row_stride + (long)h * kQD + l16 * 8) = out;
+    store_once<STREAM>(p.out[which] + (long)row * p.row_stride + (long)h * kQD + l16 * 8, out);
 }
 
 static int check_rows(const char* who, const void* k, const void* v, int64_t row_stride, const int32_t* slot_map, const void* k_cache, const void* v_cache,
@@ -225,14 +240,34 @@ static int check_rows(const char* who, const void* k, const void* v, int64_t row
     return SPEC_OK;
 }
 
+// 6 bytes are read and written per element of K and V.  Calls on three batches in turn, ordinary -> nontemporal, us: writing whole pages 49 MB 11.7 -> 12.6, 98 MB 20.5 -> 21.0, 197 MB
+// 42.4 -> 38.0, 393 MB 79.2 -> 74.6; reading rows 49 MB 10.0 -> 12.4, 98 MB 24.0 -> 21.9, 197 MB 45.1 -> 40.8, 393 MB 86.9 -> 79.2 (5 TB/s; a copy of 4 GiB reaches 4.7).
+static bool streams(int M, int Hkv) { return (size_t)M * Hkv * (6 * kQD) > kMemorySideCache * 5 / 16; }
+
+template <int TYPE, int WINDOW>
+static void launch_quantize_as(const QuantParams& p, hipStream_t s)
+{
+    const dim3 grid(((uint32_t)(p.M + WINDOW - 1) / WINDOW * (2u * (uint32_t)p.Hkv) + 3) / 4);
+    if (streams(p.M, p.Hkv)) hipLaunchKernelGGL((kv_quantize_kernel<TYPE, WINDOW, true>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((kv_quantize_kernel<TYPE, WINDOW, false>), grid, dim3(256), 0, s, p);
+}
+
+// A wave takes the runs that start in its window one by one: with windows of 16 rows whole pages keep every wave busy, with windows of 4 single rows are not in a queue.  Windows of
+// 4 / 16, us (7.5: what a call costs the host): pages of 4000 rows x heads 7.7 / 7.5, 16000 8.3 / 7.7, 32000 12.8 / 8.2, 128000 37 / 20.5; single rows, 2048 rows x heads 7.7 / 22.8, 16384
+// 20.2 / 28.5, 65536 68 / 71.  (Windows of one row: 2048 7.5, 16384 22.0, 65536 83; pages of 16000 16.9.)
 template <int TYPE>
 static void launch_quantize(const QuantParams& p, hipStream_t s)
 {
-    const uint32_t per_window = 2u * (uint32_t)p.Hkv;
-    if ((long)p.M * per_window >= 65536)
-        hipLaunchKernelGGL((kv_quantize_kernel<TYPE, 16>), dim3(((uint32_t)(p.M + 15) / 16 * per_window + 3) / 4), dim3(256), 0, s, p);
-    else
-        hipLaunchKernelGGL((kv_quantize_kernel<TYPE, 1>), dim3(((uint32_t)p.M * per_window + 3) / 4), dim3(256), 0, s, p);
+    if ((long)p.M * p.Hkv >= 24576) launch_quantize_as<TYPE, 16>(p, s);
+    else launch_quantize_as<TYPE, 4>(p, s);
+}
+
+template <int TYPE>
+static void launch_dequantize(const DequantParams& p, hipStream_t s)
+{
+    const dim3 grid((uint32_t)(((long)p.M * p.Hkv + 15) / 16), 2);
+    if (streams(p.M, p.Hkv)) hipLaunchKernelGGL((kv_dequantize_kernel<TYPE, true>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((kv_dequantize_kernel<TYPE, false>), grid, dim3(256), 0, s, p);
 }
 
 }  // namespace specv
@@ -260,8 +295,7 @@ extern "C" int spec_kv_dequantize(const void* k_cache, const void* v_cache, cons
     if (M == 0) return SPEC_OK;
     const DequantParams p{{(const uint8_t*)k_cache, (const uint8_t*)v_cache}, {k_scale, v_scale}, {(uint16_t*)k, (uint16_t*)v}, slot_map, status_flags,
                           (long)row_stride, M, Hkv, num_pages * kQP};
-    const dim3 grid((uint32_t)(((long)M * Hkv + 15) / 16), 2);
-    if (kv_type == SPEC_KV_E4M3) hipLaunchKernelGGL(kv_dequantize_kernel<SPEC_KV_E4M3>, grid, dim3(256), 0, (hipStream_t)stream, p);
-    else hipLaunchKernelGGL(kv_dequantize_kernel<SPEC_KV_INT8>, grid, dim3(256), 0, (hipStream_t)stream, p);
+    if (kv_type == SPEC_KV_E4M3) launch_dequantize<SPEC_KV_E4M3>(p, (hipStream_t)stream);
+    else launch_dequantize<SPEC_KV_INT8>(p, (hipStream_t)stream);
     return check_launch("spec_kv_dequantize");
 }

@@ -11,6 +11,7 @@
 namespace specv {
 
 constexpr int kReserveThreads = 1024;
+constexpr int kReserveDeep = 16;             // entries of a long range that a lane has in flight
 constexpr int kReserveShort = 4;             // so many table entries are looked at by the request's own thread, longer ranges by a wave
 
 struct ReserveParams {
@@ -45,13 +46,12 @@ __device__ inline ReserveRange reserve_range(const ReserveParams& p, int i)
     return q;
 }
 
-// Slot of row `row`; enters the id of a page that the row is the first of.
-__device__ inline void reserve_row(const ReserveParams& p, int row, int i, int start, int first, int place)
+// Slot of row `row` of request i, whose rows r0 .. end - 1 are positions c on; enters the id of a page that the row is the first of.
+__device__ inline void reserve_row(const ReserveParams& p, int row, int i, int r0, int end, int c, int start, int first, int place)
 {
     int slot = -1;
-    const int r0 = i >= 0 ? p.qo_indptr[i] : 0;
-    if (i >= 0 && first != kUnserved && row >= r0 && row < p.qo_indptr[i + 1]) {
-        const int pos = p.seq_lens[i] + (row - r0), g = pos / p.P, at = pos - g * p.P;
+    if (i >= 0 && first != kUnserved && row >= r0 && row < end) {
+        const int pos = c + (row - r0), g = pos / p.P, at = pos - g * p.P;
         int32_t* entry = p.page_table + (size_t)i * p.max_pages + g;
         int page;
         if (g < first) {
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
     __shared__ long wave_total[kReserveThreads / 64];
     __shared__ long block_total;
     __shared__ int s_first[kReserveThreads], s_place[kReserveThreads], s_long[kReserveThreads];
-    __shared__ int32_t s_qo[kReserveThreads];
+    __shared__ int32_t s_qo[kReserveThreads], s_end[kReserveThreads], s_c[kReserveThreads];
     __shared__ int s_longs, s_taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int count = *p.free_count;
@@ -119,20 +119,24 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
                 }
             }
             s_first[tid] = first;
+            s_qo[tid] = q.r0;
+            s_end[tid] = q.r0 + q.n;
+            s_c[tid] = q.c;
         }
         __syncthreads();
         for (int k = wave; k < s_longs; k += kReserveThreads / 64) {
             const int j = __builtin_amdgcn_readfirstlane(s_long[k]);
-            const ReserveRange w = reserve_range(p, j);
+            struct { int lo, hi; } w{s_c[j - block] / p.P, 0};
+            w.hi = (int)(((long)s_c[j - block] + (s_end[j - block] - s_qo[j - block]) + p.P - 1) / p.P);
             const int32_t* e = p.page_table + (size_t)j * p.max_pages;
             int f = w.hi, last = -1;                      // first unmapped, last mapped
             bool bad = false;
-            for (int g0 = w.lo; g0 < w.hi; g0 += 64 * 8) {
-                int page[8];
+            for (int g0 = w.lo; g0 < w.hi; g0 += 64 * kReserveDeep) {
+                int page[kReserveDeep];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) page[u] = e[min(g0 + u * 64 + lane, w.hi - 1)];
+                for (int u = 0; u < kReserveDeep; ++u) page[u] = e[min(g0 + u * 64 + lane, w.hi - 1)];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
+                for (int u = 0; u < kReserveDeep; ++u) {
                     const int g = min(g0 + u * 64 + lane, w.hi - 1);
                     if (page[u] < 0) f = min(f, g);
                     else { last = max(last, g); bad |= page[u] >= p.num_pages; }
@@ -177,7 +181,7 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
             }
             const int place = ok ? (int)(incl - need) : 0;
             first = ok ? first : kUnserved;
-            if (ROWS) { s_first[tid] = first; s_place[tid] = ok && need > 0 ? place : 0; s_qo[tid] = q.r0; }
+            if (ROWS) { s_first[tid] = first; s_place[tid] = need > 0 ? place : 0; }
             else p.req[i] = u32x2{(uint32_t)first, (uint32_t)(need > 0 ? place : 0)};
         }
         base += block_total;
@@ -192,7 +196,8 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
     if (ROWS)
         for (int row = tid; row < p.M; row += kReserveThreads) {
             const int i = reserve_request_of(s_qo, p.B, row);
-            reserve_row(p, row, i, start, i >= 0 ? s_first[i] : kUnserved, i >= 0 ? s_place[i] : 0);
+            if (i >= 0) reserve_row(p, row, i, s_qo[i], s_end[i], s_c[i], start, s_first[i], s_place[i]);
+            else p.slot_map[row] = -1;
         }
 }
 
@@ -201,8 +206,9 @@ __global__ __launch_bounds__(256) void kv_reserve_rows_kernel(ReserveParams p)
     const int row = blockIdx.x * 256 + threadIdx.x;
     if (row >= p.M) return;
     const int i = reserve_request_of(p.qo_indptr, p.B, row);
-    const u32x2 q = i >= 0 ? p.req[i] : u32x2{(uint32_t)kUnserved, 0};
-    reserve_row(p, row, i, p.hdr[0], (int)q.x, (int)q.y);
+    if (i < 0) { p.slot_map[row] = -1; return; }
+    const u32x2 q = p.req[i];
+    reserve_row(p, row, i, p.qo_indptr[i], p.qo_indptr[i + 1], p.seq_lens[i], p.hdr[0], (int)q.x, (int)q.y);
 }
 
 }  // namespace specv

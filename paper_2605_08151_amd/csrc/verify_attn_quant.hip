@@ -656,11 +656,10 @@ __global__ __launch_bounds__(256) void verify_attn_quant_merge_kernel(QuantAttnP
     for (int k = 0; k < p.B; k += 256) count += __syncthreads_count(k + tid < p.B && p.qo_indptr[k + tid] <= row);
     const int i = __builtin_amdgcn_readfirstlane(count) - 1;          // the last request that starts at or before the row
     if (i < 0) return;
+    const u32x2 q = p.req[i];                             // (not written for a request that is skipped; read with the others: one round trip)
     const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
-    if (!quant_request_ok(r0, n, c, p) || row < r0 || row >= r0 + n) return;
-    const u32x2 q = p.req[i];
     const int head = (int)q.x, pieces = (int)q.y;
-    if (pieces == 1 || hq >= p.Hq) return;                // (all of a workgroup, or it has no barrier ahead)
+    if (!quant_request_ok(r0, n, c, p) || row < r0 || row >= r0 + n || pieces == 1 || hq >= p.Hq) return;     // (all of a workgroup, or it has no barrier ahead)
     const auto slot = [&](int k) { return ((2 * (size_t)(head + k) + (k == 0)) * p.max_q_len + (row - r0)) * p.Hq + hq; };
     float mx = kNegBig, den = 0.0f;
     f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -820,7 +819,7 @@ extern "C" int spec_verify_attn_quantized(const void* q, const void* k_cache, co
     if (B > 65535 || Hkv > 65535 || M > 2147483647 / Hq) return fail(SPEC_ESHAPE, "spec_verify_attn_quantized: B, Hkv or M beyond the launch grid");
     const QuantPlan c = quant_plan(B, Hq, Hkv, max_kv_len, max_q_len);
     const size_t need = quant_workspace(c);
-    if (need > 0 && (!workspace || !aligned(workspace, 256)))
+    if (!workspace || !aligned(workspace, 256))
         return fail(SPEC_EINVAL, "spec_verify_attn_quantized: workspace is NULL or not 256-byte aligned");
     if (workspace_bytes < need)
         return fail(SPEC_EWORKSPACE, "spec_verify_attn_quantized: workspace %zu bytes, need %zu", workspace_bytes, need);

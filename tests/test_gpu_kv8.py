@@ -286,6 +286,28 @@ def test_dequantize_reads_what_the_elements_stand_for(type_, M, Hkv):
         assert (wide[:, 2 * Hkv:] == 7.0).all()
 
 
+def test_the_binding_refuses_tensors_that_do_not_fit():
+    cache, scale, slots = torch.zeros((4, 2, P, D), dtype=torch.int8, device="cuda"), torch.zeros((4, 2), device="cuda"), _i32([0, 1, 2])
+    wide = torch.zeros((3, 5, D), dtype=torch.bfloat16, device="cuda")
+    k = wide[:, :2].clone()
+    heads_apart = k.transpose(0, 1).contiguous().transpose(0, 1)
+    for k_, v_ in ((wide[:, :2], k), (heads_apart, heads_apart), (wide[:, ::2][:, :2], wide[:, ::2][:, :2]), (k.float(), k.float()), (k[:, :1], k[:, :1]), (k, k[:2])):
+        with pytest.raises(AssertionError):
+            sv.spec_kv_quantize(k_, v_, slots, cache, cache, scale, scale, None)
+        with pytest.raises(AssertionError):
+            sv.spec_kv_dequantize(cache, cache, scale, scale, slots, k_, v_, None)
+    for c, v, s in ((cache.view(torch.uint8), cache, scale), (cache, cache.view(torch.float8_e4m3fn), scale), (cache, cache[:3], scale), (cache, cache, scale[:3]),
+                    (cache, cache, scale.half()), (cache.transpose(1, 2), cache.transpose(1, 2), scale), (cache, cache, scale.cpu())):
+        with pytest.raises(AssertionError):
+            sv.spec_kv_quantize(k, k, slots, c, v, s, scale, None)
+    with pytest.raises(AssertionError):
+        sv.spec_kv_quantize(k, k, slots[:2], cache, cache, scale, scale, None)
+    with pytest.raises(sv.SpecError):                         # a row that does not begin at a multiple of 16 bytes
+        odd = torch.zeros(3 * 2 * D + 1, dtype=torch.bfloat16, device="cuda")[1:].view(3, 2, D)
+        sv.spec_kv_quantize(odd, odd, slots, cache, cache, scale, scale, None)
+    sv.spec_kv_quantize(wide[:, :2], wide[:, 2:4], slots, cache, cache.clone(), scale, scale.clone(), None)
+
+
 # ------------------------------------------------------------------------------------------------------------------
 # spec_verify_attn_quantized
 # ------------------------------------------------------------------------------------------------------------------

@@ -69,7 +69,8 @@ def test_attention_refuses(lib):
     for bad in (dict(D=64), dict(P=32), dict(Hq=9), dict(n=33), dict(n=1 << 30, Hq=2), dict(B=65536, M=65536), dict(M=1 << 29)):
         assert call(**bad) == -2, bad
     assert call(ws=None) == -1 and call(ws=ODD) == -1 and "256-byte" in _text(lib)
-    assert call(size=1000) == -3 and "workspace" in _text(lib)
+    long = dict(L=60000, width=4096)                          # (one that is cut up)
+    assert call(ws=None, **long) == -1 and call(size=1000, **long) == -3 and "workspace" in _text(lib)
     assert call(B=0, q=None) == 0 and call(M=0, q=None) == 0
     bytes_ = lib.spec_verify_attn_quantized_workspace_bytes
     assert bytes_(0, 4, 8, 2, 128, 1000, 2) == 0 and bytes_(2, 4, 9, 2, 128, 1000, 2) == 0
@@ -88,10 +89,6 @@ def test_the_binding_checks_its_tensors():
             sv.spec_kv_quantize(a["k"], k, slots, a["cache"], cache, a["scale"], scale, None)
         with pytest.raises(AssertionError):
             sv.spec_kv_dequantize(a["cache"], cache, a["scale"], scale, slots, a["k"], k, None)
-    wide = torch.zeros((3, 5, 128), dtype=torch.bfloat16)
-    for k_, v_ in ((wide[:, :2], k), (k.transpose(0, 1).contiguous().transpose(0, 1), k), (wide[:, ::2][:, :2], wide[:, ::2][:, :2])):
-        with pytest.raises(AssertionError):
-            sv._row_pair(k_, v_, 2, 128)
 
 
 def test_plain_e4m3_is_torchs():
