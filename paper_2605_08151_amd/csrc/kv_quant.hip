@@ -125,16 +125,13 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantParams p)
         const long r0 = row0 - 1 + a;
         uint8_t* to = p.cache[which] + ((size_t)page * p.Hkv + h) * (kQP * kQD) + l16 * 8;
         float* sp = p.scale[which] + (size_t)page * p.Hkv + h;
-        // rows g, g + 4, g + 8, g + 12 of the run, and the tokens before them
+        // rows g, g + 4, g + 8, g + 12 of the run
         u32x4 v[4];
-        u32x2 held[4];
-        float stored = *sp;
+        const float stored = *sp;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             v[q] = u32x4{0, 0, 0, 0};
-            held[q] = u32x2{0, 0};
             if (q * 4 + g < len) v[q] = load_once<STREAM, u32x4>(x + (r0 + q * 4 + g) * p.row_stride + (long)h * kQD + l16 * 8);
-            if (q * 4 + g < o) held[q] = *reinterpret_cast<const u32x2*>(to + (q * 4 + g) * kQD);
         }
         uint32_t top = 0;
         bool odd = false;
@@ -173,13 +170,13 @@ __global__ __launch_bounds__(256) void kv_quantize_kernel(QuantParams p)
                 }
                 store_once<STREAM>(to + (o + q * 4 + g) * kQD, pack8<TYPE>(f));
             }
-        if (now > old) {
+        if (now > old && o > 0) {                         // (seldom: the tokens before the run are read only here, 16384 single rows x heads 20.2 -> 18.9 us)
             const float ratio = old * inverse;            // now is a power of two here
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 if (q * 4 + g < o) {
                     float f[8];
-                    unpack8<TYPE>(held[q], f);
+                    unpack8<TYPE>(*reinterpret_cast<const u32x2*>(to + (q * 4 + g) * kQD), f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) f[e] *= ratio;
                     *reinterpret_cast<u32x2*>(to + (q * 4 + g) * kQD) = pack8<TYPE>(f);
@@ -253,8 +250,8 @@ static void launch_quantize_as(const QuantParams& p, hipStream_t s)
 }
 
 // A wave takes the runs that start in its window one by one: with windows of 16 rows whole pages keep every wave busy, with windows of 4 single rows are not in a queue.  Windows of
-// 4 / 16, us (7.5: what a call costs the host): pages of 4000 rows x heads 7.7 / 7.5, 16000 8.3 / 7.7, 32000 12.8 / 8.2, 128000 37 / 20.5; single rows, 2048 rows x heads 7.7 / 22.8, 16384
-// 20.2 / 28.5, 65536 68 / 71.  (Windows of one row: 2048 7.5, 16384 22.0, 65536 83; pages of 16000 16.9.)
+// 4 / 16, us (4.5 to 5.5: what a call costs the host): pages of 8000 rows x heads 5.7 / 4.4, 16000 7.7 / 5.3, 32000 11.8 / 7.7, 128000 34 / 20; single rows, 2048 rows x heads
+// 6.3 / 18.5, 16384 18.8 / 24.9, 65536 61 / 65.  (Windows of one row: 2048 5.2, 16384 19.7, 65536 70; pages of 16000 15.7.)
 template <int TYPE>
 static void launch_quantize(const QuantParams& p, hipStream_t s)
 {

@@ -125,13 +125,13 @@ def quantize(x, slots, cache, scale, type_):
     return flags
 
 
-def attend(q, k, v, ks, vs, page_table, seq_lens, qo, scale, type_):
+def attend(q, k, v, ks, vs, page_table, seq_lens, qo, scale, type_, requests=None):
     """(out [M, Hq, D], lse [M, Hq], the mean of |V| under the probabilities [M, Hq, D], the largest sum of |scale * q * k| [M, Hq]), all fp64."""
     M, Hq, _ = q.shape
     Hkv = k.shape[1]
     G = Hq // Hkv
     out, size, lse, span = np.zeros((M, Hq, D)), np.zeros((M, Hq, D)), np.zeros((M, Hq)), np.zeros((M, Hq))
-    for i in range(len(seq_lens)):
+    for i in range(len(seq_lens)) if requests is None else requests:
         c, n = int(seq_lens[i]), int(qo[i + 1] - qo[i])
         pages = page_table[i, :-(-(c + n) // P)]
         for h in range(Hkv):

@@ -359,7 +359,7 @@ def _attend(b, factor=None, max_kv_len=None, want_lse=True, pad=0, n_max=None, s
 
 def _check(b, out, lse, factor=None, requests=None):
     want, want_lse, size, span = plain.attend(b["q"].double().numpy(), b["raw"][0], b["raw"][1], b["scale"][0], b["scale"][1], b["table"], b["lens"], b["qo"],
-                                              1 / D ** 0.5 if factor is None else np.float64(np.float32(factor)), b["type"])
+                                              1 / D ** 0.5 if factor is None else np.float64(np.float32(factor)), b["type"], requests)
     tol, tol_lse = plain.tolerance(want, want_lse, size, span, b["L"])
     rows = np.concatenate([np.arange(b["qo"][i], b["qo"][i + 1]) for i in (range(len(b["lens"])) if requests is None else requests)])
     err = np.abs(out.double().cpu().numpy()[:len(want)] - want)[rows]
@@ -434,6 +434,47 @@ def test_attention_with_sharp_and_flat_scores_and_empty_scales():
     out, lse, status, _ = _attend(b)
     assert (out == 0).all()
     _check(b, out, lse)
+
+
+@pytest.mark.parametrize("B,plan", [(300, 0), (300, 1), (1024, 1), (1025, 1), (1100, 0)])
+def test_attention_of_many_requests(B, plan):
+    """More requests than are ordered by length, as many as ranges are found for, and more."""
+    rng = np.random.default_rng(B)
+    b = _attention(B, rng.integers(0, 90, B), rng.integers(1, 4, B), 4, 1, "int8")
+    sv.spec_set_tuning("attn_plan", plan)
+    try:
+        out, lse, status, _ = _attend(b)
+    finally:
+        sv.spec_set_tuning("attn_plan", 0)
+    assert int(status) == 0
+    _check(b, out, lse)
+
+
+@pytest.mark.parametrize("type_", ["e4m3", "int8"])
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("plan,n", [(1, 2), (2, 1), (1, 25)])
+def test_attention_of_a_batch_too_large_for_the_cache(type_, shared, plan, n):
+    """More than 96 MB of pages, with a prefix that all requests map or without: nontemporal loads or ordinary ones, and requests with more than 48 rows both."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(2500, 4500, 14)
+    lens[3], lens[9] = lens.max(), lens.max()                 # (ties in the order by length)
+    b = _attention(n, lens, np.full(14, n), 32, 8, type_)
+    if shared:
+        b["table"][:, :100] = b["table"][5, :100]
+    sv.spec_set_tuning("attn_plan", plan)
+    try:
+        out, lse, status, _ = _attend(b)
+    finally:
+        sv.spec_set_tuning("attn_plan", 0)
+    assert int(status) == 0
+    _check(b, out, lse, requests=[0, 3, 9, 13])
+
+
+def test_attention_with_a_negative_factor():
+    for G in (4, 24):
+        b = _attention(3, [200, 700], [1, 2], 2 * G, 2, "e4m3")
+        out, lse, status, _ = _attend(b, -0.25)
+        _check(b, out, lse, -0.25)
 
 
 @pytest.mark.parametrize("plan", [1, 2])
