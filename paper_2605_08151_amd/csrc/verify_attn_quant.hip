@@ -3,7 +3,7 @@
 //   S[t] = scale * ks[page(t)] * <q, K8_t>,  out = sum_t softmax(S)[t] * vs[page(t)] * V8_t
 //
 // The products run on the bf16 matrix cores: every e4m3 and int8 value is a bf16 value, so the conversion loses nothing, and the scales stay in fp32: K's is part of the
-// softmax scale of a page's scores, V's is a factor of the page's probabilities before they are rounded to bf16 (2^-9 each, as in spec_verify_attn).  Scores, maxima, sums and O are fp32.
+// softmax scale of a page's scores, V's is a factor of the page's probabilities before they are rounded to bf16 (with one row tile twice, the second time what the first left).  Scores, maxima, sums and O are fp32.
 //
 // HBM-bound: 256 bytes of K + V per key and kv head.
 //   Work: the batch is cut into equal ranges of work, one per workgroup and kv head, wherever the requests' borders lie, so that all workgroups are resident at once and end
@@ -410,6 +410,16 @@ struct QuantKernel {
                         const u32x4 pw = {pack_bf16x2(pr[rt][0], pr[rt][1]), pack_bf16x2(pr[rt][2], pr[rt][3]), pack_bf16x2(pr[rt][4], pr[rt][5]), pack_bf16x2(pr[rt][6], pr[rt][7])};
                         pf[rt] = __builtin_bit_cast(bf16x8, pw);
                     }
+                    // One row tile: the matrix cores have time for what the rounding left, as products of its own (error of 128 decode rows against 64 bits 0.0022 -> 0.0017, which
+                    // is the output's own rounding; 118.4 -> 119.1 us).  More tiles: once per probability, 2^-8 at most.
+                    bf16x8 rest;
+                    if constexpr (NR == 1) {
+                        u32x4 pw = __builtin_bit_cast(u32x4, pf[0]), left;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            left[k] = pack_bf16x2(pr[0][2 * k] - __builtin_bit_cast(float, pw[k] << 16), pr[0][2 * k + 1] - __builtin_bit_cast(float, pw[k] & 0xFFFF0000u));
+                        rest = __builtin_bit_cast(bf16x8, left);
+                    }
                     // ---- O^T += V^T P^T ----
                     if (wbase + 32 > kend) {
                         // slots past the range may hold anything (even NaN patterns): P is 0 there, so V must be too
@@ -442,6 +452,7 @@ struct QuantKernel {
                         const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
                         for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o[rt][t], 0, 0, 0);
+                        if constexpr (NR == 1) o[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, rest, o[0][t], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
