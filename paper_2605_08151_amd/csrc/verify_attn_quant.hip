@@ -334,26 +334,35 @@ struct QuantKernel {
                     if constexpr (NR > 1) asm volatile("" : "+v"(q_lane));
                     // ---- S^T = K Q^T; sc * ks is a score in the log2 domain ----
                     float sc[A][8];
+                    {
+                        // (a fragment of Q serves both pages, and the next one is read under its products: with a read in front of every product 32 x 2048 x 8 heads 32 us, now 29)
+                        auto q_part = [&](int rt, int s) { return __builtin_bit_cast(bf16x8, NR == 1 ? query.x[NR == 1 ? s : 0] : sQ[(rt * 4 + s) * 64 + q_lane]); };
+                        f32x4 acc[2][A];
+                        bf16x8 qx[A];
 #pragma unroll
-                    for (int pg = 0; pg < 2; ++pg) {
-                        f32x4 acc[A];
-#pragma unroll
-                        for (int rt = 0; rt < A; ++rt) acc[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                        for (int rt = 0; rt < A; ++rt) {
+                            acc[0][rt] = acc[1][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+                            qx[rt] = q_part(rt, 0);
+                        }
 #pragma unroll
                         for (int s = 0; s < 4; ++s) {
-                            const u32x4 raw = kraw[pg][s >> 1];
-                            const bf16x8 kf = (s & 1) ? bf16_oct<TYPE>(raw.z, raw.w) : bf16_oct<TYPE>(raw.x, raw.y);
+                            bf16x8 qn[A];
 #pragma unroll
-                            for (int rt = 0; rt < A; ++rt) {
-                                const bf16x8 qx = __builtin_bit_cast(bf16x8, NR == 1 ? query.x[NR == 1 ? s : 0] : sQ[(rt * 4 + s) * 64 + q_lane]);
-                                acc[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qx, acc[rt], 0, 0, 0);
+                            for (int rt = 0; rt < A; ++rt) qn[rt] = s < 3 ? q_part(rt, s + 1) : qx[rt];
+#pragma unroll
+                            for (int pg = 0; pg < 2; ++pg) {
+                                const u32x4 raw = kraw[pg][s >> 1];
+                                const bf16x8 kf = (s & 1) ? bf16_oct<TYPE>(raw.z, raw.w) : bf16_oct<TYPE>(raw.x, raw.y);
+#pragma unroll
+                                for (int rt = 0; rt < A; ++rt) acc[pg][rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qx[rt], acc[pg][rt], 0, 0, 0);
                             }
-                            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                            for (int rt = 0; rt < A; ++rt) qx[rt] = qn[rt];
                         }
 #pragma unroll
                         for (int rt = 0; rt < A; ++rt)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) sc[rt][pg * 4 + e] = acc[rt][e];
+                            for (int e = 0; e < 8; ++e) sc[rt][e] = acc[e >> 2][rt][e & 3];
                     }
                     if (wbase + 32 > min(c + 1, kend)) {  // (a scale may be 0: masked scores are scaled ones)
 #pragma unroll
@@ -386,39 +395,33 @@ struct QuantKernel {
                                 for (int t = 0; t < 8; ++t) o[rt][t] *= alpha;
                             }
                     }
-                    float pr[A][8];
+                    const bool factors = TYPE != SPEC_KV_E4M3 || vm[0] != 1.0f || vm[1] != 1.0f;
+                    bf16x8 pf[A], rest;
 #pragma unroll
                     for (int rt = 0; rt < A; ++rt) {
-                        float psum = 0.0f;
+                        float pr[8], psum = 0.0f;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             // (masked: 0, also in a row that has seen nothing, whose m_run is kNegBig)
-                            pr[rt][e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
-                            psum += pr[rt][e];
+                            pr[e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
+                            psum += pr[e];
                         }
                         l_run[rt] += psum;
-                    }
-                    if (vm[0] != 1.0f || vm[1] != 1.0f) {
+                        if (factors) {
 #pragma unroll
-                        for (int rt = 0; rt < A; ++rt)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) pr[rt][e] *= vm[e >> 2];
-                    }
-                    bf16x8 pf[A];
-#pragma unroll
-                    for (int rt = 0; rt < A; ++rt) {
-                        const u32x4 pw = {pack_bf16x2(pr[rt][0], pr[rt][1]), pack_bf16x2(pr[rt][2], pr[rt][3]), pack_bf16x2(pr[rt][4], pr[rt][5]), pack_bf16x2(pr[rt][6], pr[rt][7])};
+                            for (int e = 0; e < 8; ++e) pr[e] *= vm[e >> 2];
+                        }
+                        const u32x4 pw = {pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])};
                         pf[rt] = __builtin_bit_cast(bf16x8, pw);
-                    }
-                    // One row tile: the matrix cores have time for what the rounding left, as products of its own (error of 128 decode rows against 64 bits 0.0022 -> 0.0017, which
-                    // is the output's own rounding; 118.4 -> 119.1 us).  More tiles: once per probability, 2^-8 at most.
-                    bf16x8 rest;
-                    if constexpr (NR == 1) {
-                        u32x4 pw = __builtin_bit_cast(u32x4, pf[0]), left;
+                        // One row tile: the matrix cores have time for what the rounding left, as products of its own (error of 128 decode rows against 64 bits 0.0022 -> 0.0017, which
+                        // is the output's own rounding; 118.4 -> 119.1 us).  More tiles: once per probability, 2^-8 at most.
+                        if constexpr (NR == 1) {
+                            u32x4 left;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            left[k] = pack_bf16x2(pr[0][2 * k] - __builtin_bit_cast(float, pw[k] << 16), pr[0][2 * k + 1] - __builtin_bit_cast(float, pw[k] & 0xFFFF0000u));
-                        rest = __builtin_bit_cast(bf16x8, left);
+                            for (int k = 0; k < 4; ++k)
+                                left[k] = pack_bf16x2(pr[2 * k] - __builtin_bit_cast(float, pw[k] << 16), pr[2 * k + 1] - __builtin_bit_cast(float, pw[k] & 0xFFFF0000u));
+                            rest = __builtin_bit_cast(bf16x8, left);
+                        }
                     }
                     // ---- O^T += V^T P^T ----
                     if (wbase + 32 > kend) {
