@@ -80,6 +80,8 @@ int spec_version(void);
  *   "attn_plan"        device-built balanced work list of spec_verify_attn: 0 = automatic, 1 = always
  *                      (B <= 1024), 2 = never.
  *   "attn_plan_waves"  work items per CU that list aims at; 0 = automatic.
+ *                      (spec_verify_attn_quantized: "attn_plan" 1 = equal ranges of work, 2 = whole requests; "attn_plan_waves"
+ *                      workgroups' worth of ranges per CU; "attn_chunk" about so many keys per range.)
  *   "attn_nr3_waves"   waves per workgroup of spec_verify_attn when a request has 33..48 query rows per kv
  *                      head: 8 (default) or 4.
  *   "attn_rows"        the row-split kernel of spec_verify_attn (one 16-row tile per wave, K/V staged once per
@@ -497,10 +499,11 @@ int spec_kv_commit_tree(void* k_cache, void* v_cache, int32_t* page_table, int m
  *   c_i + j; -1 for the rows of requests that were not served and for rows of
  *   no request (r >= qo_indptr[B]).
  *   A request whose lengths do not fit (c_i < 0, n_i < 0, rows outside [0, M),
- *   more than max_pages_per_seq pages) raises SPEC_FLAG_BAD_LENGTH; one with a
- *   hole in its mapped pages, with committed tokens but no page for the last of
- *   them, or with a mapped id >= num_pages raises SPEC_FLAG_BAD_PAGE: both are
- *   not served.  A free-list entry outside [0, num_pages) is taken but not
+ *   more than max_pages_per_seq pages) raises SPEC_FLAG_BAD_LENGTH; one whose
+ *   pages from position c_i on hold a hole or an id >= num_pages, or whose first
+ *   row goes behind committed tokens of a page that is not mapped, raises
+ *   SPEC_FLAG_BAD_PAGE: both are not served (pages wholly before c_i are not
+ *   looked at).  A free-list entry outside [0, num_pages) is taken but not
  *   entered (its rows get -1) and raises SPEC_FLAG_BAD_PAGE.
  *   page_table [B, max_pages_per_seq] in/out; free_list [free_capacity] in;
  *   free_count [1] in/out; slot_map [M] out, int32.  num_pages * page_size must

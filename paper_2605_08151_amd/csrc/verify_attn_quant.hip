@@ -6,9 +6,14 @@
 // softmax scale of a page's scores, V's is a factor of the page's probabilities before they are rounded to bf16 (with one row tile twice, the second time what the first left).  Scores, maxima, sums and O are fp32.
 //
 // HBM-bound: 256 bytes of K + V per key and kv head.
-//   Work: the batch is cut into equal ranges of work, one per workgroup and kv head, wherever the requests' borders lie, so that all workgroups are resident at once and end
-//   together; a workgroup finds its range itself from the lengths (no list, no launch before it).  A request that lies in one range is finished there; pieces of others leave fp32
-//   partials, at most two per range, which a second kernel merges.
+//   Work, one of two ways (quant_plan says when):
+//   - ranges: the batch is cut into equal ranges of work, one per workgroup and kv head, wherever the requests' borders lie, so that all workgroups are resident at once and end
+//     together; a workgroup finds its range itself from the lengths (no list, no launch before it).  A request that lies in one range is finished there; pieces of others leave
+//     fp32 partials, at most two per range, which a second kernel merges.
+//   - whole requests: a workgroup per request and kv head (and row group, while those are fewer than the compute units), the longest first; nothing to merge.
+//   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 119 (5.7 TB/s); 32 x 2048 x 8, 5 rows 29 (4.7); 256 requests of 1 to 9 rows x 8
+//   117 (4.5 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 44.5 (2.3); 1 x 777 keys 10.3.  Without the arithmetic of the
+//   steps the same kernel takes 113, 26, 107, 33: what is left is the stream, the chain lengths -> page ids -> pages, and the merges.
 //   A step: a wave owns 32 keys (two pages) of every 128; its pages go straight to its own LDS (direct loads, two steps in flight: half the bytes of bf16 pages would otherwise
 //   leave HBM idle) and from there to registers.  The waves share nothing but Q until their parts are merged.
 //   Operands: scores are computed transposed (S^T = K Q^T), so that exp(S^T) is the B operand of O^T += V^T P^T.  The order of d in a score is free:
@@ -100,14 +105,15 @@ __device__ inline bool quant_request_ok(int r0, int n, int c, const QuantAttnPar
 }
 
 // Work of one step of a request with `rows` query rows per kv head: a pass over the keys per kQuantTiles row tiles, and the tiles' products (128 keys in a full CU
-// took 1.44, 1.60, 1.95 us with 1, 2, 3 tiles).
+// took 1.33, 1.56, 1.82 us with 1, 2, 3 tiles).
 __host__ __device__ constexpr int quant_step_work(int rows)
 {
     const int tiles = (rows + 15) / 16;
     return (tiles + kQuantTiles - 1) / kQuantTiles * 4 + tiles;
 }
 
-// ... and of a piece besides its steps: its first pages' round trip, the merge of its waves
+// ... and of a piece besides its steps: its first pages' round trip, the merge of its waves (0 / 20 / 40: 256 mixed requests 132.8 / 128.0 / 130.2 us, 8 x 32-64k 46.4 / 45.0 / 45.8,
+// 128 decode rows x 8 heads as ranges 125.8 / 128.1 / 130.8)
 __host__ __device__ constexpr int quant_piece_work(int rows) { return ((rows + 15) / 16 + kQuantTiles - 1) / kQuantTiles * 20; }
 
 // One piece: keys kbeg .. kend (kbeg a multiple of 128) of request i for one kv head.
