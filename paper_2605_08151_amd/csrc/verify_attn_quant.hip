@@ -12,8 +12,8 @@
 //     fp32 partials, at most two per range, which a second kernel merges.
 //   - whole requests: a workgroup per request and kv head (and row group, while those are fewer than the compute units), the longest first; nothing to merge.
 //   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 119 (5.7 TB/s); 32 x 2048 x 8, 5 rows 29 (4.7); 256 requests of 1 to 9 rows x 8
-//   117 (4.5 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 44.5 (2.3); 1 x 777 keys 10.3.  Without the arithmetic of the
-//   steps the same kernel takes 113, 26, 107, 33: what is left is the stream, the chain lengths -> page ids -> pages, and the merges.
+//   115 (4.6 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 42.5 (2.4); 1 x 777 keys 10.3.  Without the arithmetic of the
+//   steps an earlier form that took 119, 32, 118, 45 took 113, 26, 107, 33: what is left is the stream, the chain lengths -> page ids -> pages, and the merges.
 //   A step: a wave owns 32 keys (two pages) of every 128; its pages go straight to its own LDS (direct loads, two steps in flight: half the bytes of bf16 pages would otherwise
 //   leave HBM idle) and from there to registers.  The waves share nothing but Q until their parts are merged.
 //   Operands: scores are computed transposed (S^T = K Q^T), so that exp(S^T) is the B operand of O^T += V^T P^T.  The order of d in a score is free:
@@ -268,6 +268,8 @@ struct QuantKernel {
         if (steps_of(u) > 0) issue(stream, pages.id, 0);
         pages = load_scales(u, 0, pages.id);
         Query query = load_q(u, group);
+        if (steps_of(u) > 1) issue(stream, pages.id, 1);
+        bool first = true;
 
         while (true) {
             const int first_row = group * kQuantTiles * 16, R = min(p.G * u.n - first_row, NR * 16), c = u.c, kend = u.kend, steps = steps_of(u);
@@ -277,7 +279,8 @@ struct QuantKernel {
             }
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // the first step's pages, with the scales and queries that were requested beside them
             Scales now = scales_of(pages, 0), nxt = scales_of(pages, 1);
-            if (steps > 1) issue(stream, pages.id, 1);
+            if (steps > 1 && !first) issue(stream, pages.id, 1);           // (the first piece's is on its way, since nothing is merged in its place: 8 x 32-64k 43.9 -> 42.5 us)
+            first = false;
             if constexpr (NR > 1) __syncthreads();
             // what comes next, and its page ids
             QuantPiece v = u;
@@ -589,8 +592,9 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
         // Every request's work and what comes before it, four requests per thread; the total gives the size of a range, and the request in which this one starts leaves its
         // number and place in LDS.
         constexpr int kPer = kQuantListed / kQuantThreads;
-        int* s_scan = reinterpret_cast<int*>(smem);       // [4], then {request, work before it}
+        int* s_scan = reinterpret_cast<int*>(smem);       // [4], then {request, work before it, its first row, rows, committed tokens}
         int work[kPer], mine = 0;
+        QuantRequest request[kPer];
         bool bad = false;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
@@ -598,6 +602,7 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
             work[k] = 0;
             if (i < p.B) {
                 const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
+                request[k] = QuantRequest{r0, n, c};
                 if (quant_request_ok(r0, n, c, p)) work[k] = quant_piece_work(p.G * n) + (c + n + kQuantStep - 1) / kQuantStep * quant_step_work(p.G * n);
                 else bad = true;
             }
@@ -624,16 +629,26 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
         if (first >= total) return;
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
-            if (first >= before && first < before + work[k]) { s_scan[4] = tid * kPer + k; s_scan[5] = before; }
+            if (first >= before && first < before + work[k]) {
+                s_scan[4] = tid * kPer + k;
+                s_scan[5] = before;
+                s_scan[6] = request[k].r0;
+                s_scan[7] = request[k].n;
+                s_scan[8] = request[k].c;
+            }
             before += work[k];
         }
         __syncthreads();
         int i = __builtin_amdgcn_readfirstlane(s_scan[4]), at = __builtin_amdgcn_readfirstlane(s_scan[5]);      // request, and the work before it
+        QuantRequest known{__builtin_amdgcn_readfirstlane(s_scan[6]), __builtin_amdgcn_readfirstlane(s_scan[7]), __builtin_amdgcn_readfirstlane(s_scan[8])};
+        bool start = true;                                // (the first request's fields are here: a round trip less, 256 mixed requests 117.4 -> 114.8 us)
         __syncthreads();                                  // (pages land there next)
         // the next request with steps in this range, whole or in part
         auto piece_from = [&](QuantPiece& u) {
             while (at < last) {
-                const auto [r0, n, c] = quant_request(p, i);
+                if (!start) known = quant_request(p, i);
+                start = false;
+                const auto [r0, n, c] = known;
                 if (quant_request_ok(r0, n, c, p)) {
                     const int len = c + n, steps = (len + kQuantStep - 1) / kQuantStep, w = quant_step_work(p.G * n);
                     // the steps whose place lies in this range
