@@ -687,14 +687,26 @@ __global__ __launch_bounds__(256) void verify_attn_quant_merge_kernel(QuantAttnP
     __shared__ float s_den[kGroups], s_max[kGroups];
     const int row = blockIdx.x, tid = threadIdx.x, grp = tid >> 5, d4 = (tid & 31) * 4;
     const int hq = HEADS == 1 ? blockIdx.y : blockIdx.y * 8 + grp;
-    int count = 0;
-    for (int k = 0; k < p.B; k += 256) count += __syncthreads_count(k + tid < p.B && p.qo_indptr[k + tid] <= row);
-    const int i = __builtin_amdgcn_readfirstlane(count) - 1;          // the last request that starts at or before the row
-    if (i < 0) return;
-    const u32x2 q = p.req[i];                             // (not written for a request that is skipped; read with the others: one round trip)
-    const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
-    const int head = (int)q.x, pieces = (int)q.y;
-    if (!quant_request_ok(r0, n, c, p) || row < r0 || row >= r0 + n || pieces == 1 || hq >= p.Hq) return;     // (all of a workgroup, or it has no barrier ahead)
+    // The row's request: every request's fields are read at once, with where its pieces are (not written for one that is skipped), so that the partials are one more round trip
+    // away and not two (13 ragged requests 20.7 -> 20.3 us, 8 x 32-64k 42.7 -> 42.2).
+    __shared__ int s_last, s_req[3];
+    if (tid == 0) s_last = -1;
+    __syncthreads();
+    int mine = -1, r0 = 0;
+    u32x2 where = {0, 0};
+    for (int i = tid; i < p.B; i += 256) {
+        const int at = p.qo_indptr[i], n = p.qo_indptr[i + 1] - at, c = p.seq_lens[i];
+        const u32x2 q = p.req[i];
+        if (quant_request_ok(at, n, c, p) && row >= at && row < at + n) { mine = i; r0 = at; where = q; }
+    }
+    if (mine >= 0) atomicMax(&s_last, mine);              // (one thread, unless the row ranges overlap)
+    __syncthreads();
+    if (mine >= 0 && mine == s_last) { s_req[0] = r0; s_req[1] = (int)where.x; s_req[2] = (int)where.y; }
+    __syncthreads();
+    if (s_last < 0) return;
+    const int head = __builtin_amdgcn_readfirstlane(s_req[1]), pieces = __builtin_amdgcn_readfirstlane(s_req[2]);
+    r0 = __builtin_amdgcn_readfirstlane(s_req[0]);
+    if (pieces == 1 || hq >= p.Hq) return;                // (all of a workgroup, or it has no barrier ahead)
     const auto slot = [&](int k) { return ((2 * (size_t)(head + k) + (k == 0)) * p.max_q_len + (row - r0)) * p.Hq + hq; };
     float mx = kNegBig, den = 0.0f;
     f32x4 num = f32x4{0.f, 0.f, 0.f, 0.f};
