@@ -560,8 +560,8 @@ int spec_kv_dequantize(const void* k_cache, const void* v_cache, const float* k_
 
 /* spec_verify_attn_quantized — spec_verify_attn over a cache in 8 bits: the same operation (K_t and V_t are the values
  * that the elements stand for; scales: any finite values >= 0), arguments, limits, flags and errors.  Products in bf16 (every element is
- * a bf16 value), scales, scores, sums and accumulation in fp32; the probabilities, times V's scale's fraction, are rounded to bf16
- * (with at most 16 query rows per kv head to the sum of two bf16 numbers).
+ * a bf16 value), scales, scores, sums and accumulation in fp32; the probabilities, times V's scale's fraction, are rounded to the sum
+ * of two bf16 numbers (2^-16).
  * Chains only: candidate trees need the bf16 cache.  At the positions that a request sees no element may be NaN (spec_kv_quantize
  * writes none); the slots behind them, and unmapped pages' scales, may hold anything. */
 size_t spec_verify_attn_quantized_workspace_bytes(int B, int M, int Hq, int Hkv, int D, int max_kv_len, int max_q_len);

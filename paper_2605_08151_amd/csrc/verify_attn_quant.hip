@@ -3,7 +3,9 @@
 //   S[t] = scale * ks[page(t)] * <q, K8_t>,  out = sum_t softmax(S)[t] * vs[page(t)] * V8_t
 //
 // The products run on the bf16 matrix cores: every e4m3 and int8 value is a bf16 value, so the conversion loses nothing, and the scales stay in fp32: K's is part of the
-// softmax scale of a page's scores, V's is a factor of the page's probabilities before they are rounded to bf16 (with one row tile twice, the second time what the first left).  Scores, maxima, sums and O are fp32.
+// softmax scale of a page's scores, V's is a factor of the page's probabilities.  Those enter the products as the sum of two bf16 numbers, the second being what the rounding to the first
+// left: 2^-16 of a probability is lost, and the output's own rounding is what remains of the error (32 x 2048 keys, 5 rows against 64 bits: 0.0022 with one bf16 number, 0.0017 with two, as an
+// fp32 form has; 28.6 -> 30.2 us, 256 mixed requests 115 -> 128, 8 x 32-64k 41.4 -> 43.6).  Scores, maxima, sums and O are fp32.
 //
 // HBM-bound: 256 bytes of K + V per key and kv head.
 //   Work, one of two ways (quant_plan says when):
@@ -11,8 +13,8 @@
 //     together; a workgroup finds its range itself from the lengths (no list, no launch before it).  A request that lies in one range is finished there; pieces of others leave
 //     fp32 partials, at most two per range, which a second kernel merges.
 //   - whole requests: a workgroup per request and kv head (and row group, while those are fewer than the compute units), the longest first; nothing to merge.
-//   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 119 (5.7 TB/s); 32 x 2048 x 8, 5 rows 29 (4.7); 256 requests of 1 to 9 rows x 8
-//   115 (4.6 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 42.5 (2.4); 1 x 777 keys 10.3.  Without the arithmetic of the
+//   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 119 (5.7 TB/s); 32 x 2048 x 8, 5 rows 30 (4.6); 256 requests of 1 to 9 rows x 8
+//   128 (4.1 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 43.6 (2.3); 1 x 777 keys 10.3.  Without the arithmetic of the
 //   steps an earlier form that took 119, 32, 118, 45 took 113, 26, 107, 33: what is left is the stream, the chain lengths -> page ids -> pages, and the merges.
 //   A step: a wave owns 32 keys (two pages) of every 128; its pages go straight to its own LDS (direct loads, two steps in flight: half the bytes of bf16 pages would otherwise
 //   leave HBM idle) and from there to registers.  The waves share nothing but Q until their parts are merged.
@@ -405,7 +407,7 @@ struct QuantKernel {
                             }
                     }
                     const bool factors = TYPE != SPEC_KV_E4M3 || vm[0] != 1.0f || vm[1] != 1.0f;
-                    bf16x8 pf[A], rest;
+                    bf16x8 pf[A], rest[A];
 #pragma unroll
                     for (int rt = 0; rt < A; ++rt) {
                         float pr[8], psum = 0.0f;
@@ -422,15 +424,12 @@ struct QuantKernel {
                         }
                         const u32x4 pw = {pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]), pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])};
                         pf[rt] = __builtin_bit_cast(bf16x8, pw);
-                        // One row tile: the matrix cores have time for what the rounding left, as products of its own (error of 128 decode rows against 64 bits 0.0022 -> 0.0017, which
-                        // is the output's own rounding; 118.4 -> 119.1 us).  More tiles: once per probability, 2^-8 at most.
-                        if constexpr (NR == 1) {
-                            u32x4 left;
+                        // What the rounding left is rounded in turn and has products of its own: 2^-16 of a probability is lost.
+                        u32x4 left;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                left[k] = pack_bf16x2(pr[2 * k] - __builtin_bit_cast(float, pw[k] << 16), pr[2 * k + 1] - __builtin_bit_cast(float, pw[k] & 0xFFFF0000u));
-                            rest = __builtin_bit_cast(bf16x8, left);
-                        }
+                        for (int k = 0; k < 4; ++k)
+                            left[k] = pack_bf16x2(pr[2 * k] - __builtin_bit_cast(float, pw[k] << 16), pr[2 * k + 1] - __builtin_bit_cast(float, pw[k] & 0xFFFF0000u));
+                        rest[rt] = __builtin_bit_cast(bf16x8, left);
                     }
                     // ---- O^T += V^T P^T ----
                     if (wbase + 32 > kend) {
@@ -464,7 +463,8 @@ struct QuantKernel {
                         const bf16x8 vf = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
                         for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o[rt][t], 0, 0, 0);
-                        if constexpr (NR == 1) o[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, rest, o[0][t], 0, 0, 0);
+#pragma unroll
+                        for (int rt = 0; rt < A; ++rt) o[rt][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, rest[rt], o[rt][t], 0, 0, 0);
                         __builtin_amdgcn_sched_barrier(0);
                     }
                 }
