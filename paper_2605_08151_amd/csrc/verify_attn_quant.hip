@@ -22,6 +22,7 @@
 //   K: lane (l16, g) holds key l16, d = 32 g .. + 31: MFMA s contracts d = 32 g + 8 s .. + 7, and Q is laid out alike;
 //   V: lane (l16, g) holds d = 8 l16 .. + 7 of keys 4 g .. 4 g + 3: byte t of the four rows, paired by v_perm, converts to the A operand of output tile t, whose rows are
 //      d = 8 m + t.  A lane then ends with d = 32 g .. 32 g + 31 of its query row.
+#include "attn_request.h"
 #include "common.h"
 #include "kv_stream.h"
 
@@ -103,7 +104,7 @@ __device__ inline bf16x8 bf16_oct(uint32_t a, uint32_t b)
 
 __device__ inline bool quant_request_ok(int r0, int n, int c, const QuantAttnParams& p)
 {
-    return n >= 1 && n <= p.max_q_len && r0 >= 0 && r0 + n <= p.M && c >= 0 && c + n <= p.max_kv_len;
+    return attn_request_fits(r0, n, c, p.M, p.max_q_len, p.max_kv_len);
 }
 
 // Work of one step of a request with `rows` query rows per kv head: a pass over the keys per kQuantTiles row tiles, and the tiles' products (128 keys in a full CU
@@ -133,7 +134,7 @@ __device__ inline int scalar_load(const int32_t* x, int i)
 __device__ inline QuantRequest quant_request(const QuantAttnParams& p, int i)
 {
     const int r0 = scalar_load(p.qo_indptr, i);
-    return {r0, scalar_load(p.qo_indptr, i + 1) - r0, scalar_load(p.seq_lens, i)};
+    return {r0, attn_request_rows(r0, scalar_load(p.qo_indptr, i + 1)), scalar_load(p.seq_lens, i)};
 }
 
 // An address that is the same in every lane, in scalar registers whatever the compiler makes of what it is computed from.  The s_nop is the distance that a load written
@@ -601,7 +602,7 @@ __global__ __launch_bounds__(kQuantThreads, kQuantWgsPerCu) void verify_attn_qua
             const int i = tid * kPer + k;
             work[k] = 0;
             if (i < p.B) {
-                const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
+                const int r0 = p.qo_indptr[i], n = attn_request_rows(r0, p.qo_indptr[i + 1]), c = p.seq_lens[i];
                 request[k] = QuantRequest{r0, n, c};
                 if (quant_request_ok(r0, n, c, p)) work[k] = quant_piece_work(p.G * n) + (c + n + kQuantStep - 1) / kQuantStep * quant_step_work(p.G * n);
                 else bad = true;
@@ -695,7 +696,7 @@ __global__ __launch_bounds__(256) void verify_attn_quant_merge_kernel(QuantAttnP
     int mine = -1, r0 = 0;
     u32x2 where = {0, 0};
     for (int i = tid; i < p.B; i += 256) {
-        const int at = p.qo_indptr[i], n = p.qo_indptr[i + 1] - at, c = p.seq_lens[i];
+        const int at = p.qo_indptr[i], n = attn_request_rows(at, p.qo_indptr[i + 1]), c = p.seq_lens[i];
         const u32x2 q = p.req[i];
         if (quant_request_ok(at, n, c, p) && row >= at && row < at + n) { mine = i; r0 = at; where = q; }
     }
