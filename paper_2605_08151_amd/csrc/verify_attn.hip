@@ -18,6 +18,7 @@
 //   Every chunk writes an unnormalised fp32 partial (O, running max, sum); a second kernel merges the
 //   partials of a row in split order (deterministic) and writes bf16.
 #include "attn_lds.h"
+#include "attn_request.h"
 #include "batch_rules.h"
 #include "common.h"
 #include "kv_stream.h"
@@ -93,7 +94,7 @@ __device__ inline void kv_scan(const AttnParams& p, int i, int page, bool total_
 
 __device__ inline bool request_ok(int r0, int n, int c, const AttnParams& p)
 {
-    return n >= 1 && n <= p.max_q_len && r0 >= 0 && r0 + n <= p.M && c >= 0 && c + n <= p.max_kv_len;
+    return attn_request_fits(r0, n, c, p.M, p.max_q_len, p.max_kv_len);
 }
 
 // Request number `rank` in the order of committed keys, longest first (ties: request order), and its metadata.  A lane per request (at most 64); one memory round trip,
@@ -113,7 +114,7 @@ __device__ inline RequestRef longest_first(const AttnParams& p, int rank)
     for (int k = 0; k < 64; ++k) above += (uint32_t)__builtin_amdgcn_readlane((int)key, k) > key;
     const int i = __ffsll((long long)__ballot(above == rank)) - 1;
     const int r0 = __builtin_amdgcn_readlane(q0, i);
-    return {i, r0, __builtin_amdgcn_readlane(q1, i) - r0, __builtin_amdgcn_readlane(c, i)};
+    return {i, r0, attn_request_rows(r0, __builtin_amdgcn_readlane(q1, i)), __builtin_amdgcn_readlane(c, i)};
 }
 
 // NR: 16-row query tiles per (request, kv head); NW: waves per workgroup (each owns 32 keys of a step);
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(NW * 64) void verify_attn_kernel(AttnParams p)
         i = q.i; r0 = q.r0; n = q.n; c = q.c;
     } else {
         r0 = p.qo_indptr[i];
-        n = p.qo_indptr[i + 1] - r0;
+        n = attn_request_rows(r0, p.qo_indptr[i + 1]);
         c = p.seq_lens[i];
     }
     if (!request_ok(r0, n, c, p)) {
@@ -594,7 +595,7 @@ __global__ __launch_bounds__(NW * 64, (NW <= 5 ? 4 : (NW == 6 ? 3 : 2))) void ve
         i = q.i; r0 = q.r0; n = q.n; c = q.c;
     } else {
         r0 = p.qo_indptr[i];
-        n = p.qo_indptr[i + 1] - r0;
+        n = attn_request_rows(r0, p.qo_indptr[i + 1]);
         c = p.seq_lens[i];
     }
     if (!request_ok(r0, n, c, p)) {
@@ -872,7 +873,7 @@ __global__ __launch_bounds__(1024) void verify_attn_plan_kernel(AttnParams p, in
     int len = 0, n = 0, bad = 0;
     if (tid < B) {
         const int r0 = p.qo_indptr[tid];
-        n = p.qo_indptr[tid + 1] - r0;
+        n = attn_request_rows(r0, p.qo_indptr[tid + 1]);
         const int c = p.seq_lens[tid];
         if (request_ok(r0, n, c, p)) len = c + n; else { bad = 1; n = 0; }
     }
@@ -985,7 +986,7 @@ __global__ __launch_bounds__(256) void verify_attn_combine_kernel(AttnParams p, 
     const int row = blockIdx.x, hq = blockIdx.y, tid = threadIdx.x, grp = tid >> 5, d4 = (tid & 31) * 4;
     const int i = request_of_row(p, B, row);
     if (i < 0) return;
-    const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
+    const int r0 = p.qo_indptr[i], n = attn_request_rows(r0, p.qo_indptr[i + 1]), c = p.seq_lens[i];
     if (!request_ok(r0, n, c, p) || row < r0 || row >= r0 + n) return;
     const int len = c + n;
     const int ns = p.plan_req ? p.plan_req[2 * i] : (len + p.chunk_target - 1) / p.chunk_target;
@@ -1023,7 +1024,7 @@ __global__ __launch_bounds__(256) void verify_attn_combine_rows_kernel(AttnParam
     const int row = blockIdx.x, tid = threadIdx.x, hq = blockIdx.y * 8 + (tid >> 5), d4 = (tid & 31) * 4;
     const int i = request_of_row(p, B, row);
     if (i < 0 || hq >= p.Hq) return;
-    const int r0 = p.qo_indptr[i], n = p.qo_indptr[i + 1] - r0, c = p.seq_lens[i];
+    const int r0 = p.qo_indptr[i], n = attn_request_rows(r0, p.qo_indptr[i + 1]), c = p.seq_lens[i];
     if (!request_ok(r0, n, c, p) || row < r0 || row >= r0 + n) return;
     const int len = c + n;
     const int ns = p.plan_req ? p.plan_req[2 * i] : (len + p.chunk_target - 1) / p.chunk_target;

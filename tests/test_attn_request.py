@@ -55,7 +55,7 @@ def test_what_fits_is_what_fits_in_whole_numbers(rule):
 
 
 def test_no_kernel_has_a_rule_of_its_own():
-    for name in ("verify_attn_quant.hip",):
+    for name in ("verify_attn.hip", "verify_attn_quant.hip"):
         text = open(os.path.join(CSRC, name)).read()
         assert "attn_request_fits(" in text and "attn_request_rows(" in text, name
         assert "c + n <= p.max_kv_len" not in text and "r0 + n <= p.M" not in text, name

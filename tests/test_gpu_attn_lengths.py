@@ -1,8 +1,9 @@
 """Committed lengths and row offsets at the end of 32 bits: the request is skipped and flagged, the others are computed."""
 import numpy as np
 import pytest
+import torch
 
-from test_gpu_kv8 import _attend, _attention, _check, sv
+from test_gpu_kv8 import D, P, _attend, _attention, _check, _i32, sv
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,34 @@ def test_quantized_attention_skips_offsets_that_pass_32_bits(plan, far):
     assert int(status) == sv.FLAG_BAD_LENGTH
     assert (out[qo[1]:qo[3]] == 77.0).all() and (lse[qo[1]:qo[3]] == 77.0).all()
     _check(b, out, lse, requests=[0, 3])
+
+
+@pytest.mark.parametrize("far", [TOP, TOP - 1])
+@pytest.mark.parametrize("n,G", [(1, 4), (5, 8), (16, 8)])
+@pytest.mark.parametrize("chunk,plan,rows", [(0, 0, 0), (256, 2, 0), (0, 1, 0), (256, 2, 1), (256, 2, 2)])
+def test_bf16_attention_skips_lengths_that_pass_32_bits(far, n, G, chunk, plan, rows):
+    """The same bits as with a negative length in their place: nothing is written for such a request, and the others are cut up alike."""
+    rng = np.random.default_rng(n)
+    lens, Hkv, pages = [300, far, 700, 90, far], 2, 200
+    cache = [torch.from_numpy(rng.normal(0, 1, (pages, Hkv, P, D))).to(torch.bfloat16).cuda() for _ in range(2)]
+    q = torch.from_numpy(rng.normal(0, 1, (5 * n, Hkv * G, D))).to(torch.bfloat16).cuda()
+    table, qo = _i32(rng.permutation(pages)[:5 * 40].reshape(5, 40)), _i32(np.arange(6) * n)
+    table = torch.cat([table, table.flip(0)], 1).contiguous()
+    got = []
+    for name, value in (("attn_chunk", chunk), ("attn_plan", plan), ("attn_rows", rows)):
+        sv.spec_set_tuning(name, value)
+    try:
+        for far_ in (-1, far):
+            status = _i32([0])
+            out, lse = torch.full_like(q, 77.0), torch.full((5 * n, Hkv * G), 77.0, device="cuda")
+            ws = torch.zeros(max(256, sv.spec_verify_attn_workspace_bytes(5, 5 * n, Hkv * G, Hkv, D, 1000, n)), dtype=torch.uint8, device="cuda")
+            sv.spec_verify_attn(q, *cache, table, _i32([far_ if c == far else c for c in lens]), qo, out, lse, 1000, n, 0.09, status, ws)
+            assert int(status) == sv.FLAG_BAD_LENGTH
+            got.append((out, lse))
+    finally:
+        for name in ("attn_chunk", "attn_plan", "attn_rows"):
+            sv.spec_set_tuning(name, 0)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+        for i in range(5):
+            assert (b[i * n:(i + 1) * n] == 77.0).all() == (lens[i] == far)
