@@ -498,12 +498,14 @@ int spec_kv_commit_tree(void* k_cache, void* v_cache, int32_t* page_table, int m
  *   slot_map[r], for row r = qo_indptr[i] + j: page * P + offset of position
  *   c_i + j; -1 for the rows of requests that were not served and for rows of
  *   no request (r >= qo_indptr[B]).
- *   A request whose lengths do not fit (c_i < 0, n_i < 0, rows outside [0, M),
- *   more than max_pages_per_seq pages) raises SPEC_FLAG_BAD_LENGTH; one whose
- *   pages from position c_i on hold a hole or an id >= num_pages, or whose first
- *   row goes behind committed tokens of a page that is not mapped, raises
+ *   A request whose lengths do not fit (c_i < 0, rows outside [0, M), more than
+ *   max_pages_per_seq pages) raises SPEC_FLAG_BAD_LENGTH; one whose pages from
+ *   position c_i on hold a hole or an id >= num_pages, or whose first row goes
+ *   behind committed tokens of a page that is not mapped, raises
  *   SPEC_FLAG_BAD_PAGE: both are not served (pages wholly before c_i are not
- *   looked at).  A free-list entry outside [0, num_pages) is taken but not
+ *   looked at).  With offsets that descend anywhere (n_i < 0) no request of the
+ *   call is served, SPEC_FLAG_BAD_LENGTH.
+ *   A free-list entry outside [0, num_pages) is taken but not
  *   entered (its rows get -1) and raises SPEC_FLAG_BAD_PAGE.
  *   page_table [B, max_pages_per_seq] in/out; free_list [free_capacity] in;
  *   free_count [1] in/out; slot_map [M] out, int32.  num_pages * page_size must

@@ -30,7 +30,7 @@ struct ReserveParams {
 constexpr int kUnserved = 0x7FFFFFFF;
 
 // What a request asks for; ok: its lengths fit the table and the row range.
-struct ReserveRange { int lo, hi, c, r0, n; bool ok; };
+struct ReserveRange { int lo, hi, c, r0, n; bool ok, descends; };
 
 __device__ inline ReserveRange reserve_range(const ReserveParams& p, int i)
 {
@@ -39,6 +39,7 @@ __device__ inline ReserveRange reserve_range(const ReserveParams& p, int i)
     const long end = p.qo_indptr[i + 1], n = end - q.r0;
     q.c = p.seq_lens[i];
     q.n = (int)n;
+    q.descends = n < 0;
     const long len = q.c + n, hi = (len + p.P - 1) / p.P;
     q.ok = n >= 0 && q.c >= 0 && q.r0 >= 0 && end <= p.M && len <= 0x7FFFFFFFL && (n == 0 || hi <= p.max_pages);
     q.lo = q.ok ? q.c / p.P : 0;
@@ -81,7 +82,7 @@ __device__ inline int reserve_request_of(const int32_t* qo, int B, int row)
     return lo;
 }
 
-// ROWS: at most 1024 requests, whose rows this workgroup does as well.
+// ROWS: at most 1024 requests (one block), whose rows this workgroup does as well.
 template <bool ROWS>
 __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReserveParams p)
 {
@@ -96,11 +97,18 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
     if (tid == 0) s_taken = 0;
     long base = 0;
     int flags = 0;
+    // Offsets that descend can give a row to two requests, of which the search finds one: the other's pages would be taken and not entered.  So nobody is served then.  (Up to
+    // 1024 requests are looked at below, in their only block.)
+    int descends = 0;
+    if constexpr (!ROWS) {
+        for (int i = tid; i < p.B; i += kReserveThreads) descends |= p.qo_indptr[i + 1] < p.qo_indptr[i];
+        descends = __syncthreads_or(descends);
+    }
     for (int block = 0; block < p.B; block += kReserveThreads) {
         if (tid == 0) s_longs = 0;
         __syncthreads();                                  // (also: the arrays of the block before have been read)
         const int i = block + tid;
-        ReserveRange q{0, 0, 0, 0, 0, false};
+        ReserveRange q{0, 0, 0, 0, 0, false, false};
         bool ok = false;
         int first = 0;
         if (i < p.B) {
@@ -123,7 +131,8 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
             s_end[tid] = q.r0 + q.n;
             s_c[tid] = q.c;
         }
-        __syncthreads();
+        if constexpr (ROWS) descends = __syncthreads_or(q.descends);
+        else __syncthreads();
         for (int k = wave; k < s_longs; k += kReserveThreads / 64) {
             const int j = __builtin_amdgcn_readfirstlane(s_long[k]);
             struct { int lo, hi; } w{s_c[j - block] / p.P, 0};
@@ -152,6 +161,7 @@ __global__ __launch_bounds__(kReserveThreads) void kv_reserve_kernel(ReservePara
             if (first < 0) ok = false;
             if (ok && q.n > 0 && q.c % p.P != 0 && first == q.lo) ok = false;     // the page of its last tokens is not there
             if (!ok && q.ok) flags |= SPEC_FLAG_BAD_PAGE;
+            if (descends) { ok = false; flags |= SPEC_FLAG_BAD_LENGTH; }
         }
         const long need = i < p.B && ok ? q.hi - first : 0;
         long incl = need;
