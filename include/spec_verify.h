@@ -566,6 +566,7 @@ int spec_kv_dequantize(const void* k_cache, const void* v_cache, const float* k_
  * of two bf16 numbers (2^-16).
  * Chains only: candidate trees need the bf16 cache.  At the positions that a request sees no element may be NaN (spec_kv_quantize
  * writes none); the slots behind them, and unmapped pages' scales, may hold anything. */
+/* Bytes for a call of these heads with at most so many requests and bounds at most as large: one workspace for a server's largest batch serves every smaller one. */
 size_t spec_verify_attn_quantized_workspace_bytes(int B, int M, int Hq, int Hkv, int D, int max_kv_len, int max_q_len);
 
 int spec_verify_attn_quantized(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,

@@ -770,6 +770,16 @@ struct QuantPlan {
 
 constexpr int kQuantMinSteps = 2;            // of a range
 
+// Ranges of a call at most, whatever its lengths: by the compute units (or the keys per range that are asked for), and by the work at its bounds, for which a request's piece
+// work counts as four steps (it is 20 / 5 of one with one row tile, less with more).  Grows with B and max_kv_len alone.
+static long quant_most_ranges(int B, int Hkv, int max_kv_len)
+{
+    const int chunk = g_attn_chunk_override, waves = g_attn_plan_waves;
+    const long steps = ((long)max_kv_len + kQuantStep - 1) / kQuantStep, least = chunk > 0 ? 1 : kQuantMinSteps;
+    const long ranges = chunk > 0 ? (long)B * max_kv_len / chunk + 1 : std::max<long>(1, (long)device_cu_count() * (waves > 0 ? waves : kQuantWgsPerCu) / Hkv);
+    return std::min(std::min(ranges, (B * (steps + 4) + least - 1) / least), 8192L);
+}
+
 static QuantPlan quant_plan(int B, int Hq, int Hkv, int max_kv_len, int max_q_len)
 {
     QuantPlan c{};
@@ -779,7 +789,7 @@ static QuantPlan quant_plan(int B, int Hq, int Hkv, int max_kv_len, int max_q_le
     const long cus = device_cu_count(), units = (long)B * Hkv;
     c.groups = units >= cus ? 1 : row_groups;
     c.by_length = B > 1 && B <= kQuantOrdered && units > cus;
-    const int mode = g_attn_plan, chunk = g_attn_chunk_override, waves = g_attn_plan_waves;
+    const int mode = g_attn_plan, chunk = g_attn_chunk_override;
     const long steps = ((long)max_kv_len + kQuantStep - 1) / kQuantStep, work = quant_step_work(G * max_q_len);
     const long most = B * (steps * work + quant_piece_work(G * max_q_len));            // work of the batch at its bounds
     if (mode == 2 || B > kQuantListed || most > (1L << 30)) return c;
@@ -792,10 +802,8 @@ static QuantPlan quant_plan(int B, int Hq, int Hkv, int max_kv_len, int max_q_le
     const double one_us = steps * (NR == 1 ? 0.8 : NR == 2 ? 1.3 : 1.6 * row_groups);
     const double saved_us = 8.0 + (NR == 1 ? 0.0 : 10.0 * std::min(1.0, all_us / 15.0));
     if (mode != 1 && chunk <= 0 && one_us <= saved_us + 0.5 * all_us) return c;
-    c.min_work = (int)(kQuantMinSteps * work);
-    long ranges = std::max<long>(1, cus * (waves > 0 ? waves : kQuantWgsPerCu) / Hkv);
-    if (chunk > 0) { ranges = (long)B * max_kv_len / chunk + 1; c.min_work = (int)work; }
-    ranges = std::min(std::min<long>(ranges, (most + c.min_work - 1) / c.min_work), 8192L);
+    c.min_work = (int)((chunk > 0 ? 1 : kQuantMinSteps) * work);
+    const long ranges = std::min(quant_most_ranges(B, Hkv, max_kv_len), (most + c.min_work - 1) / c.min_work);
     c.ranges = (int)ranges;
     c.many = ranges > 16L * B;
     c.slots = 2 * (size_t)ranges * max_q_len * Hq;
@@ -836,8 +844,14 @@ extern "C" size_t spec_verify_attn_quantized_workspace_bytes(int B, int M, int H
 {
     using namespace specv;
     (void)D;
-    if (B <= 0 || M <= 0 || Hq <= 0 || Hkv <= 0 || max_kv_len <= 0 || Hq % Hkv != 0) return 0;
-    return quant_workspace(quant_plan(B, Hq, Hkv, max_kv_len, max_q_len > 0 ? max_q_len : 1));
+    if (B <= 0 || M <= 0 || Hq <= 0 || Hkv <= 0 || max_kv_len <= 0 || Hq % Hkv != 0 || g_attn_plan == 2) return 0;
+    // Also where this batch is taken as whole requests: a smaller one may be cut.
+    QuantPlan c{};
+    B = std::min(B, kQuantListed);
+    c.ranges = (int)quant_most_ranges(B, Hkv, max_kv_len);
+    c.slots = 2 * (size_t)c.ranges * (max_q_len > 0 ? max_q_len : 1) * Hq;
+    c.req_bytes = round_up((size_t)B * 8, 256);
+    return quant_workspace(c);
 }
 
 extern "C" int spec_verify_attn_quantized(const void* q, const void* k_cache, const void* v_cache, const float* k_scale, const float* v_scale,
