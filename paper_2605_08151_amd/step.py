@@ -43,6 +43,7 @@ class VerifyStep:
         # pages and slots of the step's rows, and attention over a cache in 8 bits
         self.slot_map = torch.full((M,), -1, dtype=torch.int32, device=dev)
         self.reserve_ws = torch.empty(max(256, sv.spec_kv_reserve_workspace_bytes(B)), dtype=torch.uint8, device=dev)
+        self.quantized_ws = None
         if quantized_cache:
             self.quantized_ws = torch.empty(max(256, sv.spec_verify_attn_quantized_workspace_bytes(B, M, Hq, Hkv, D, max_kv_len, gamma_max + 1)),
                                             dtype=torch.uint8, device=dev)
@@ -58,6 +59,7 @@ class VerifyStep:
 
     def attn_quantized(self, q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, scale, want_lse=True):
         """attn() over a cache in 8 bits (VerifyStep(..., quantized_cache=True))."""
+        assert self.quantized_ws is not None, "attn_quantized() needs VerifyStep(..., quantized_cache=True), which allocates its workspace"
         sv.spec_verify_attn_quantized(q, k_cache, v_cache, k_scale, v_scale, page_table, seq_lens, qo_indptr, self.attn_out,
                                       self.lse if want_lse else None, self.max_kv_len, self.gamma_max + 1, scale, self.status, self.quantized_ws)
         return self.attn_out

@@ -62,3 +62,10 @@ def test_one_workspace_serves_smaller_batches():
         sv.spec_verify_attn_quantized(*args[:-1], ws)
         assert int(status) == 0
         _check(b, out, lse)
+
+
+def test_a_step_without_the_workspace_says_so():
+    from paper_2605_08151_amd.step import VerifyStep
+    step = VerifyStep(1, 1, 8, 1, 128, 64, 64, 0, 100, device="cpu")
+    with pytest.raises(AssertionError, match="quantized_cache=True"):
+        step.attn_quantized(*[None] * 9)
