@@ -561,7 +561,7 @@ int spec_kv_dequantize(const void* k_cache, const void* v_cache, const float* k_
                        int M, int Hkv, int D, int page_size, int kv_type, int32_t* status_flags, void* stream);
 
 /* spec_verify_attn_quantized — spec_verify_attn over a cache in 8 bits: the same operation (K_t and V_t are the values
- * that the elements stand for; scales: any finite values >= 0), arguments, limits, flags and errors.  Products in bf16 (every element is
+ * that the elements stand for; scales: any finite values >= 0 for which scores and 64 times the sum of a request's |V| are finite in fp32), arguments, limits, flags and errors.  Products in bf16 (every element is
  * a bf16 value), scales, scores, sums and accumulation in fp32; the probabilities, times V's scale's fraction, are rounded to the sum
  * of two bf16 numbers (2^-16).
  * Chains only: candidate trees need the bf16 cache.  At the positions that a request sees no element may be NaN (spec_kv_quantize

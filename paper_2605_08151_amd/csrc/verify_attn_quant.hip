@@ -49,8 +49,8 @@ constexpr int kQuantOrdered = kQuantThreads;             // whole requests are t
 constexpr int kQuantPageBytes = kP * kD;
 constexpr int kQuantStageBytes = 4 * kQuantPageBytes;    // two pages of K, two of V
 constexpr int kQuantWaveBytes = kQuantStages * kQuantStageBytes;
-constexpr float kNegBig = -1.0e30f;          // "nothing seen yet" running maximum (log2 domain)
-constexpr float kMasked = -2.0e30f;          // a masked score: 0 in the exponential below every maximum
+constexpr float kNegBig = -3.4028235e38f;    // "nothing seen yet" running maximum (log2 domain): below every score
+constexpr float kMasked = -INFINITY;         // a masked score: 0 in the exponential below every maximum
 constexpr float kMaxSlack = 6.0f;            // how far a score may exceed the reference before a rescale
 
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));    // (rows of the output may start at any element)
@@ -332,8 +332,7 @@ struct QuantKernel {
                         for (int r = 0; r < 4; ++r) vraw[pg][r] = *reinterpret_cast<const u32x2*>(sK + (2 + pg) * kQuantPageBytes + (4 * g + r) * kD + l16 * 8);
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    float ks[2] = {now.ks[0], now.ks[1]};
-                    const float vm[2] = {now.vm[0], now.vm[1]}, ve[2] = {now.ve[0], now.ve[1]};
+                    const float ks[2] = {now.ks[0], now.ks[1]}, vm[2] = {now.vm[0], now.vm[1]}, ve[2] = {now.ve[0], now.ve[1]};
                     now = nxt;
                     if (step + 2 < steps) {
                         if (((step + 2) & 31) == 0) pages = load_scales(u, step + 2, load_ids(u, step + 2));     // the next 32 steps
@@ -344,9 +343,12 @@ struct QuantKernel {
                     // (two row tiles and more: Q is read again in every step; the compiler would rather keep all of it in registers)
                     int q_lane = lane;
                     if constexpr (NR > 1) asm volatile("" : "+v"(q_lane));
-                    // ---- S^T = K Q^T; sc * ks is a score in the log2 domain ----
+                    // ---- S^T = K Q^T; scores in the log2 domain ----
                     float sc[A][8];
                     {
+                        // (a score is rounded before the maximum is taken and before it is subtracted: a product fused with the subtraction would exceed its own maximum by what the
+                        // rounding lost, 2^8 where scores are 2^32)
+#pragma clang fp contract(off)
                         // (a fragment of Q serves both pages, and the next one is read under its products: with a read in front of every product 32 x 2048 x 8 heads 32 us, now 29)
                         auto q_part = [&](int rt, int s) { return __builtin_bit_cast(bf16x8, NR == 1 ? query.x[NR == 1 ? s : 0] : sQ[(rt * 4 + s) * 64 + q_lane]); };
                         f32x4 acc[2][A];
@@ -374,15 +376,14 @@ struct QuantKernel {
 #pragma unroll
                         for (int rt = 0; rt < A; ++rt)
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) sc[rt][e] = acc[e >> 2][rt][e & 3];
+                            for (int e = 0; e < 8; ++e) sc[rt][e] = acc[e >> 2][rt][e & 3] * ks[e >> 2];
                     }
-                    if (wbase + 32 > min(c + 1, kend)) {  // (a scale may be 0: masked scores are scaled ones)
+                    if (wbase + 32 > min(c + 1, kend)) {
 #pragma unroll
                         for (int rt = 0; rt < A; ++rt)
 #pragma unroll
                             for (int e = 0; e < 8; ++e)
-                                sc[rt][e] = wbase + (e >> 2) * 16 + g * 4 + (e & 3) < limit[rt] ? sc[rt][e] * ks[e >> 2] : kMasked;
-                        ks[0] = ks[1] = 1.0f;
+                                sc[rt][e] = wbase + (e >> 2) * 16 + g * 4 + (e & 3) < limit[rt] ? sc[rt][e] : kMasked;
                     }
                     // The reference maximum moves only when a score exceeds it by more than kMaxSlack, so exp2(s - m_run) <= 2^kMaxSlack stays well inside fp32 and bf16 and O
                     // is rescaled a handful of times (the result is the same softmax: O and l carry the same factor).  A lane looks at its own 8 scores, and the four
@@ -391,8 +392,7 @@ struct QuantKernel {
                     bool grow = false;
 #pragma unroll
                     for (int rt = 0; rt < A; ++rt) {
-                        const float a = fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])), b = fmaxf(fmaxf(sc[rt][4], sc[rt][5]), fmaxf(sc[rt][6], sc[rt][7]));
-                        tmax[rt] = fmaxf(a * ks[0], b * ks[1]);
+                        tmax[rt] = fmaxf(fmaxf(fmaxf(sc[rt][0], sc[rt][1]), fmaxf(sc[rt][2], sc[rt][3])), fmaxf(fmaxf(sc[rt][4], sc[rt][5]), fmaxf(sc[rt][6], sc[rt][7])));
                         grow |= tmax[rt] > m_run[rt] + kMaxSlack;
                     }
                     if (__any(grow)) {
@@ -415,7 +415,7 @@ struct QuantKernel {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             // (masked: 0, also in a row that has seen nothing, whose m_run is kNegBig)
-                            pr[e] = __builtin_amdgcn_exp2f(fmaf(sc[rt][e], ks[e >> 2], -m_run[rt]));
+                            pr[e] = __builtin_amdgcn_exp2f(sc[rt][e] - m_run[rt]);
                             psum += pr[e];
                         }
                         l_run[rt] += psum;
