@@ -3,6 +3,7 @@
 // target's critical path, so the kernels are plain: one workgroup per request, coalesced token reads.
 #include "batch_rules.h"
 #include "common.h"
+#include "kv_pages.h"
 
 namespace specv {
 
@@ -68,9 +69,9 @@ __global__ __launch_bounds__(kTruncThreads) void kv_truncate_kernel(
                 live = true;
                 const int k = keep_len[i];
                 new_len = k < 0 ? 0 : (k > c ? c : k);
-                had = (c + P - 1) / P;
+                had = pages_of(c, P);
                 if (had > max_pages) had = max_pages;
-                keep = (new_len + P - 1) / P;
+                keep = pages_of(new_len, P);
                 for (int pg = keep; pg < had; ++pg)
                     nfree += page_table[(size_t)i * max_pages + pg] >= 0;
             } else {

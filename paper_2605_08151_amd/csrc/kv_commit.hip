@@ -5,6 +5,7 @@
 // block scan of "pages this request frees" gives every request its slot range in the free list,
 // so the list order is request-ascending then logical-page-ascending whatever the thread timing.
 #include "common.h"
+#include "kv_pages.h"
 
 namespace specv {
 
@@ -27,16 +28,16 @@ __global__ __launch_bounds__(kCommitThreads) void kv_commit_kernel(
         int keep = 0, had = 0, new_len = 0, nfree = 0;
         bool live = false;
         if (i < B) {
-            const int n = qo_indptr[i + 1] - qo_indptr[i];
+            const int n = kv_rows(qo_indptr[i], qo_indptr[i + 1]);
             const int c = seq_lens[i];
-            if (n >= 1 && c >= 0) {
+            if (kv_length_fits(n, c)) {
                 live = true;
                 int a = accept_len[i];
                 a = a < 0 ? 0 : (a > n - 1 ? n - 1 : a);
                 new_len = c + a + 1;
-                had = (c + n + P - 1) / P;
+                had = pages_of(c + n, P);
                 if (had > max_pages) had = max_pages;
-                keep = (new_len + P - 1) / P;
+                keep = pages_of(new_len, P);
                 for (int pg = keep; pg < had; ++pg)
                     nfree += page_table[(size_t)i * max_pages + pg] >= 0;
             } else {
@@ -94,8 +95,8 @@ __global__ __launch_bounds__(256) void kv_gather_path_kernel(
     const int32_t* __restrict__ path, int gamma_max, int num_pages, int Hkv, int D, int P, int32_t* __restrict__ status_flags)
 {
     const int i = blockIdx.x, tid = threadIdx.x;
-    const int n = qo_indptr[i + 1] - qo_indptr[i], c = seq_lens[i];
-    if (n < 1 || c < 0) return;                           // the commit kernel flags it
+    const int n = kv_rows(qo_indptr[i], qo_indptr[i + 1]), c = seq_lens[i];
+    if (!kv_length_fits(n, c)) return;                    // the commit kernel flags it
     int a = accept_len[i];
     a = a < 0 ? 0 : (a > n - 1 ? n - 1 : a);
     const int chunks = Hkv * (D / 8);                     // 16-byte pieces of one position's K (and of its V)
@@ -107,7 +108,8 @@ __global__ __launch_bounds__(256) void kv_gather_path_kernel(
             return;
         }
         if (src != dst) {
-            const int ps = page_table[(size_t)i * max_pages + src / P], pd = page_table[(size_t)i * max_pages + dst / P];
+            const bool inside = src / P < max_pages;      // (dst < src)
+            const int ps = inside ? page_table[(size_t)i * max_pages + src / P] : -1, pd = inside ? page_table[(size_t)i * max_pages + dst / P] : -1;
             if (ps < 0 || ps >= num_pages || pd < 0 || pd >= num_pages) {
                 if (tid == 0 && status_flags) atomicOr(status_flags, SPEC_FLAG_BAD_PAGE);
                 return;
