@@ -252,6 +252,7 @@ static void launch_quantize_as(const QuantParams& p, hipStream_t s)
 // A wave takes the runs that start in its window one by one: with windows of 16 rows whole pages keep every wave busy, with windows of 4 single rows are not in a queue.  Windows of
 // 4 / 16, us (4.5 to 5.5: what a call costs the host): pages of 8000 rows x heads 5.7 / 4.4, 16000 7.7 / 5.3, 32000 11.8 / 7.7, 128000 34 / 20; single rows, 2048 rows x heads
 // 6.3 / 18.5, 16384 18.8 / 24.9, 65536 61 / 65.  (Windows of one row: 2048 5.2, 16384 19.7, 65536 70; pages of 16000 15.7.)
+// The rule goes by rows x heads, which is all that the host knows of them, and is drawn for pages: single rows pay for it behind the line.
 template <int TYPE>
 static void launch_quantize(const QuantParams& p, hipStream_t s)
 {

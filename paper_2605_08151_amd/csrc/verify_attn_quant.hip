@@ -5,7 +5,7 @@
 // The products run on the bf16 matrix cores: every e4m3 and int8 value is a bf16 value, so the conversion loses nothing, and the scales stay in fp32: K's is part of the
 // softmax scale of a page's scores, V's is a factor of the page's probabilities.  Those enter the products as the sum of two bf16 numbers, the second being what the rounding to the first
 // left: 2^-16 of a probability is lost, and the output's own rounding is what remains of the error (32 x 2048 keys, 5 rows against 64 bits: 0.0022 with one bf16 number, 0.0017 with two, as an
-// fp32 form has; 28.6 -> 30.2 us, 256 mixed requests 115 -> 128, 8 x 32-64k 41.4 -> 43.6).  Scores, maxima, sums and O are fp32.
+// fp32 form has; 28.6 -> 30.2 us, 256 mixed requests 115 -> 125, 8 x 32-64k 41.4 -> 43.6).  Scores, maxima, sums and O are fp32.
 //
 // HBM-bound: 256 bytes of K + V per key and kv head.
 //   Work, one of two ways (quant_plan says when):
@@ -13,8 +13,8 @@
 //     together; a workgroup finds its range itself from the lengths (no list, no launch before it).  A request that lies in one range is finished there; pieces of others leave
 //     fp32 partials, at most two per range, which a second kernel merges.
 //   - whole requests: a workgroup per request and kv head (and row group, while those are fewer than the compute units), the longest first; nothing to merge.
-//   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 119 (5.7 TB/s); 32 x 2048 x 8, 5 rows 30 (4.6); 256 requests of 1 to 9 rows x 8
-//   128 (4.1 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 43.6 (2.3); 1 x 777 keys 10.3.  Without the arithmetic of the
+//   Calls, us (bytes of K and V at the rate over the call): 128 x 2.6k keys x 8 heads, 1 row 118 (5.7 TB/s); 32 x 2048 x 8, 5 rows 30.6 (4.5); 256 requests of 1 to 9 rows x 8
+//   125 (4.3 with the second pass over the keys of those with more than 48 rows); 8 x 32-64k in int8, 5 rows x 8 44 (2.3); 1 x 777 keys 10.1.  Without the arithmetic of the
 //   steps an earlier form that took 119, 32, 118, 45 took 113, 26, 107, 33: what is left is the stream, the chain lengths -> page ids -> pages, and the merges.
 //   A step: a wave owns 32 keys (two pages) of every 128; its pages go straight to its own LDS (direct loads, two steps in flight: half the bytes of bf16 pages would otherwise
 //   leave HBM idle) and from there to registers.  The waves share nothing but Q until their parts are merged.
@@ -108,15 +108,15 @@ __device__ inline bool quant_request_ok(int r0, int n, int c, const QuantAttnPar
 }
 
 // Work of one step of a request with `rows` query rows per kv head: a pass over the keys per kQuantTiles row tiles, and the tiles' products (128 keys in a full CU
-// took 1.33, 1.56, 1.82 us with 1, 2, 3 tiles).
+// take 1.31, 1.32, 1.48, 2.92, 4.70 us with 1, 2, 3, 4, 8 tiles: up to 3 the stream bounds an even batch; in one where it does not they take 0.95, 1.36, 1.65).
 __host__ __device__ constexpr int quant_step_work(int rows)
 {
     const int tiles = (rows + 15) / 16;
     return (tiles + kQuantTiles - 1) / kQuantTiles * 4 + tiles;
 }
 
-// ... and of a piece besides its steps: its first pages' round trip, the merge of its waves (0 / 20 / 40: 256 mixed requests 132.8 / 128.0 / 130.2 us, 8 x 32-64k 46.4 / 45.0 / 45.8,
-// 128 decode rows x 8 heads as ranges 125.8 / 128.1 / 130.8)
+// ... and of a piece besides its steps: its first pages' round trip, the merge of its waves (0 / 20 / 40: 256 mixed requests 139 / 125 / 123 us, 8 x 32-64k 48 / 45 / 44,
+// 128 decode rows x 8 heads as ranges 129 / 132 / 134)
 __host__ __device__ constexpr int quant_piece_work(int rows) { return ((rows + 15) / 16 + kQuantTiles - 1) / kQuantTiles * 20; }
 
 // One piece: keys kbeg .. kend (kbeg a multiple of 128) of request i for one kv head.
@@ -795,9 +795,11 @@ static QuantPlan quant_plan(int B, int Hq, int Hkv, int max_kv_len, int max_q_le
     if (mode == 2 || B > kQuantListed || most > (1L << 30)) return c;
     // Whole requests need no merge and leave no bubbles between pieces, but the longest one is as long as the call.  In us: what it takes (0.8, 1.3, 1.6 a step with 1, 2, 3 row
     // tiles) against what the ranges' second launch and partials cost (8, with more than one row tile 18 once the chip is busy) and half of what the batch takes at its bounds and
-    // 6.5 TB/s (lengths are usually below them).  Ranges / whole, us, all requests at the bound | lengths from an eighth of it on, 1 row tile: 1 x 1024 keys 13.1 / 12.0, 2048 14.0 / 18.4;
-    // 128 requests x heads of 2048 24.4 / 20.6 | 20.0 / 19.5, 4096 34.9 / 34.7 | 25.7 / 32.6; 256 of 4096 57.5 / 48.1 | 38.3 / 35.2, 8192 101 / 90 | 63 / 66; 3 row tiles: 1 x 512
-    // 17.3 / 15.0, 1024 17.5 / 21.4; 128 of 2048 37.1 / 37.0 | 30.4 / 35.1; 256 of 2048 51.6 / 40.6 | 40.5 / 38.0, 4096 78 / 67 | 56 / 63.
+    // 6.5 TB/s (lengths are usually below them).  Ranges / whole, us, all requests at the bound | lengths from an eighth of it on, 1 row tile: 1 x 1024 keys 11.3 / 11.3, 2048 12.3 / 18.5;
+    // 128 requests x heads of 2048 21.6 / 20.5 | 19.0 / 20.2, 4096 31.9 / 35.4 | 23.9 / 34.7; 256 of 4096 55.6 / 46.5 | 36.8 / 36.8, 8192 98.5 / 87.1 | 62.2 / 68.8; 3 row tiles: 1 x 512
+    // 15.1 / 13.4, 1024 15.4 / 19.9; 128 of 2048 37.7 / 36.0 | 30.9 / 35.7; 256 of 2048 51.7 / 38.5 | 43.5 / 37.6, 4096 77 / 66 | 58 / 63.
+    // The bounds are all that the host knows.  Where they say little the rule is off: 32 requests of 2048 keys x 8 heads, 5 rows take 32 us whole under a bound of 2053 and 40 as
+    // ranges under one of 4096 or more; one request of 65000 keys among 127 of 1024, 1 row x 8 heads, bound 65536, takes 496 whole, which the rule chooses, and 84 as ranges.
     const double all_us = (double)units * max_kv_len * (2 * kD) / 6.5e6;
     const double one_us = steps * (NR == 1 ? 0.8 : NR == 2 ? 1.3 : 1.6 * row_groups);
     const double saved_us = 8.0 + (NR == 1 ? 0.0 : 10.0 * std::min(1.0, all_us / 15.0));
