@@ -541,7 +541,8 @@ int spec_kv_reserve(int32_t* page_table, int max_pages_per_seq, int num_pages,
  *   o tokens before the run are rounded again (element * (old / new) in fp32); the
  *   slots behind the run are left as they were.  So a page begins anew with its slot
  *   0, and rows that verification rejected are overwritten by the next ones, but what
- *   they did to the scale of a page that still holds tokens stays.
+ *   they did to the scale of a page that still holds tokens, and by that to those
+ *   tokens, stays: later output can depend on what the draft proposed.
  *   Infinities and NaN are stored as 0, do not count for the scale, and raise
  *   SPEC_FLAG_BAD_KV.  A page that occurs in more than one run of a call, and
  *   slots that occur twice, end with unspecified contents (nothing else is touched).
